@@ -39,6 +39,16 @@ flp_status fll_add_rmsnorm(int32_t dtype, void* resid, const void* delta, const 
 flp_status fll_rope(int32_t dtype, void* q, void* k, const int32_t* positions, int32_t n_tokens, int32_t n_q_heads,
                     int32_t n_kv_heads, int32_t head_dim, float theta, void* hip_stream);
 
+/* Norms of queries and keys per head with the rotary embedding behind them, for models that normalise both: of every head's
+ * row x [head_dim], r = x / sqrt(mean(x^2) + eps) * w (w_q for queries, w_k for keys, [head_dim], shared by the heads), then r
+ * rotated as fll_rope does; rounded once.  q_in and k_in: rows of n_q_heads / n_kv_heads heads, ld_* elements apart (they may be parts of
+ * one fused product's rows, 16-byte aligned); q_out [n_tokens, n_q_heads, head_dim] and k_out [n_tokens, n_kv_heads, head_dim]
+ * dense.  Either side may be left out (q_in or k_in NULL).  q_out may be q_in, and k_out k_in, where the rows are dense; otherwise
+ * outputs overlap no input.  May be captured into a HIP graph. */
+flp_status fll_qk_norm_rope(int32_t dtype, const void* q_in, int64_t ld_q_in, const void* k_in, int64_t ld_k_in, const void* w_q,
+                            const void* w_k, const int32_t* positions, void* q_out, void* k_out, int32_t n_tokens,
+                            int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float eps, float theta, void* hip_stream);
+
 /* out = gate * sigmoid(gate) * up, element-wise over [n_tokens, width]; ld_* = elements between rows
  * (gate and up may be the two halves of one [n_tokens, 2 * width] tensor).  out may be gate. */
 flp_status fll_silu_mul(int32_t dtype, const void* gate, int64_t ld_gate, const void* up, int64_t ld_up, void* out,

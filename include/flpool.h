@@ -148,6 +148,53 @@ flp_status flp_kv_append(flp_pool* pool, const flp_attn_batch* batch, void* hip_
 flp_status flp_paged_prefix_attention(flp_pool* pool, const flp_attn_batch* batch, void* hip_stream);
 
 /* ---------------------------------------------------------------------------
+ * KV cache in 8 bits.  In a 16-bit pool a block may hold K and V as e4m3 (4 exponent bits, 3 mantissa bits, largest value
+ * 448, no infinities): flp_pool_kv8_block_tokens() = 2 * block_tokens positions in the same bytes, K of (kv head g, slot s,
+ * channel c) at byte (g*pb + s)*d + c, V at n_kv*pb*d + (g*d + c)*pb + s with pb positions per block.  A stored byte stands
+ * for its e4m3 value times the scale of its kv head, one for K and one for V.  Which sequences are held so is the caller's
+ * business: blocks of both kinds, and LoRA pages, lie in one pool, and swaps move them alike.  In the calls below
+ * position p of sequence i lives in block block_tables[i][p / pb], slot p % pb, and the limits on lengths go by pb.
+ * fp32 pools: FLP_ENOTSUP.
+ *
+ * These calls (and the tree and accept calls further down) allocate nothing and keep no state where their batch has up to 96
+ * sequences with new tokens and no context is cut into pieces; such a call can be captured into a HIP graph and replayed. A call
+ * that needs a staging slot or the pool's workspace is refused under capture (FLP_ENOTSUP).  The pool's device must be
+ * the current one (FLP_EINVAL). */
+typedef struct {
+  const float* k_scale;           /* device float[n_kv_heads], finite and > 0                 */
+  const float* v_scale;           /* device float[n_kv_heads], finite and > 0                 */
+} flp_kv8_scales;
+
+int64_t flp_pool_kv8_block_tokens(const flp_pool* pool);   /* 0: the pool holds no 8-bit cache */
+
+/* Quantise the new tokens' K and V into their slots: the byte is x / scale in fp32, limited to [-448, 448] (infinities
+ * too), rounded to e4m3 to nearest even; a NaN stays NaN.  Every other slot keeps what it holds.  Arguments as for flp_kv_append. */
+flp_status flp_kv_append8(flp_pool* pool, const flp_attn_batch* batch, const flp_kv8_scales* scales, void* hip_stream);
+
+/* flp_paged_prefix_attention over such a cache; with k_new and v_new flp_kv_append8 is enqueued first (the new tokens attend
+ * over their own K and V as stored). */
+flp_status flp_paged_prefix_attention8(flp_pool* pool, const flp_attn_batch* batch, const flp_kv8_scales* scales,
+                                       void* hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Trees of drafted tokens (speculative decoding: several continuations of a sequence are verified in one step).  The new tokens
+ * of a sequence, at most 64 (FLP_ERANGE), are the nodes of its tree and lie at positions prefix_len[i] + j in the order they come.
+ * New token j sees every position of the prefix and those new tokens j' of its sequence whose bit j' is set in
+ * tree_mask[cu_new[i] + j]: its ancestors and, as a rule, itself.  Bits at or past the number of new tokens are ignored; a token that sees
+ * nothing (no prefix, no bit) gets zeros.  What K and V of positions that a token does not see hold, infinities and NaN
+ * included, does not reach its row.  Otherwise as flp_paged_prefix_attention (scales == NULL: the cache has the pool's type)
+ * or flp_paged_prefix_attention8.  tree_mask: device uint64[T], 8-byte aligned. */
+flp_status flp_paged_tree_attention(flp_pool* pool, const flp_attn_batch* batch, const uint64_t* tree_mask,
+                                    const flp_kv8_scales* scales, void* hip_stream);
+
+/* Keep the accepted path of each sequence's tree: K and V of position prefix_len[i] + path[cu_new[i] + j] move to position
+ * prefix_len[i] + j for j < n_accept[i].  The path is increasing, so path[cu_new[i] + j] >= j; an entry outside
+ * [0, number of new tokens) ends it.  Uses cu_new, prefix_len and block_tables of the batch.  kv8: the cache is in 8 bits.
+ * n_accept: device int32[n_seqs], path: device int32[T] (both may be results of earlier work on the stream). */
+flp_status flp_kv_accept(flp_pool* pool, const flp_attn_batch* batch, const int32_t* n_accept, const int32_t* path, int32_t kv8,
+                         void* hip_stream);
+
+/* ---------------------------------------------------------------------------
  * Batched heterogeneous LoRA (Eq. 1 and Eq. 2 in row-vector form; section 2.1:
  * queries with different adapters run in one batch).  Token t carries adapter
  * a = token_adapter[t]; for every projection p of the batch

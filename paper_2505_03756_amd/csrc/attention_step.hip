@@ -1,0 +1,590 @@
+// Paged attention of the calls that add to flp_paged_prefix_attention: new tokens over a cache held in e4m3, and trees of up to 64
+// drafted tokens over a cache of any type.
+//
+// For query row r = (new token, query head of kv head g):  out_r = v_scale sum_k w_rk V_k,  w_r = softmax over the k that r sees of
+// (sm_scale k_scale) q_r . K_k.  A token sees every position of the prefix; of its sequence's new tokens those up to itself, or
+// those whose bit is set in its mask.  A row that sees nothing is zero.
+//
+// One wave owns 16 J rows of one (sequence, kv head) and walks tiles of the context with a running maximum and sum.  K and V go from
+// memory to registers 16 bytes per lane and are used there for all rows; nothing is staged.  S^T = K Q^T and O^T = V^T W^T with
+// 16x16 instructions: a lane holds one query row (column l % 16) of every row tile and the RUN = 16 bytes / element size consecutive
+// positions from RUN (l / 16) on, because row m of key tile t is key RUN (m / 4) + 4 t + m % 4; these positions are also its 16-byte
+// run of the transposed V.  Which channels a step of the scores takes is free as long as K and Q agree, so that a lane's 16 bytes of
+// K are one step in 16 bits, two in 8, four (16x16x4) in fp32.
+//
+//   fp32     fp32 instructions throughout.
+//   16 bit   weights in two pieces of the pool's type, the value and its remainder: 16 bits of them in bf16 and 22 in fp16, where one
+//            piece would add an error as large as the rounding of the result.  An infinite V would meet a negative remainder, so the
+//            words of V are looked over first and what is not finite goes another way (below).
+//   8 bit    e4m3 is exact in fp16 and in bf16: K is widened to the type of q, V and the weights to fp16, two pieces as well.
+//
+// A workgroup is four waves: row tiles x slices of the context, so that waves of different row tiles read the same K and V at about
+// the same time, and slices are merged in LDS.  Long contexts of small launches are cut into pieces over workgroups as well, which
+// a second launch merges in piece order.  Bound by the traffic of K and V up to 32 rows or so per kv head.
+//
+// Infinities and NaN in V reach the rows that see them and no others: in the tiles where some row does not see everything, and in
+// all tiles of 16-bit V, values that are not finite are replaced by zero, and whether a row sees one is counted with products of
+// indicators.  Slots past the end of a sequence hold arbitrary bits and are replaced, never multiplied.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "flp_internal.h"
+#include "flp_types.h"
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ f32x4 mma(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(h16x8 a, h16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(b16x8 a, b16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+template <typename V>
+__device__ __forceinline__ V bits_as(u32x4 r) {
+  V v;
+  __builtin_memcpy(&v, &r, 16);
+  return v;
+}
+__device__ __forceinline__ h16x8 widen(uint32_t lo, uint32_t hi, h16x8*) {
+  h16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true),
+                __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true)};
+  h16x8 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+__device__ __forceinline__ b16x8 widen(uint32_t lo, uint32_t hi, b16x8*) {
+  b16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true),
+                __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true)};
+  b16x8 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+
+template <typename S, bool KV8>
+struct Kind {                                          // 16-bit cache
+  typedef typename std::conditional<std::is_same<S, F16>::value, h16x8, b16x8>::type kvec;
+  typedef kvec vvec;
+  static constexpr int ES = 2, STEPS = 1, PIECES = 2;
+  static __device__ __forceinline__ kvec k(u32x4 raw, int) { return bits_as<kvec>(raw); }
+  static __device__ __forceinline__ vvec v(u32x4 raw, int) { return bits_as<vvec>(raw); }
+  static __device__ __forceinline__ uint32_t odd(uint32_t w) {       // high bits set where a value is not finite
+    return std::is_same<S, F16>::value ? ((w & 0x7fff7fffu) + 0x04000400u) & 0x80008000u : ((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+  }
+};
+template <typename S>
+struct Kind<S, true> {                                 // e4m3 cache
+  typedef typename std::conditional<std::is_same<S, F16>::value, h16x8, b16x8>::type kvec;
+  typedef h16x8 vvec;
+  static constexpr int ES = 1, STEPS = 2, PIECES = 2;
+  static __device__ __forceinline__ kvec k(u32x4 raw, int s) { return widen(raw[2 * s], raw[2 * s + 1], (kvec*)nullptr); }
+  static __device__ __forceinline__ vvec v(u32x4 raw, int s) { return widen(raw[2 * s], raw[2 * s + 1], (vvec*)nullptr); }
+  static __device__ __forceinline__ uint32_t odd(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+};
+template <>
+struct Kind<F32, false> {
+  typedef float kvec;
+  typedef float vvec;
+  static constexpr int ES = 4, STEPS = 4, PIECES = 1;
+  static __device__ __forceinline__ float k(u32x4 raw, int s) { return __uint_as_float(raw[s]); }
+  static __device__ __forceinline__ float v(u32x4 raw, int s) { return __uint_as_float(raw[s]); }
+  static __device__ __forceinline__ uint32_t odd(uint32_t w) { return ((w & 0x7fffffffu) + 0x00800000u) & 0x80000000u; }
+};
+
+// element e of a step's operand
+__device__ __forceinline__ void put(float& v, int, float x) { v = x; }
+__device__ __forceinline__ void put(h16x8& v, int e, float x) { v[e] = (_Float16)x; }
+__device__ __forceinline__ void put(b16x8& v, int e, float x) { v[e] = (__bf16)x; }
+__device__ __forceinline__ float got(float v, int) { return v; }
+__device__ __forceinline__ float got(h16x8 v, int e) { return (float)v[e]; }
+__device__ __forceinline__ float got(b16x8 v, int e) { return (float)v[e]; }
+
+// The record that workgroup unit `u` belongs to: the last one whose first unit is not behind u
+__device__ __forceinline__ int find(const FlpStepSeq* __restrict__ recs, int n, int u, int FlpStepSeq::*first) {
+  int at = -1;
+  for (int base = 0; base < n; base += 64) {
+    const int i = base + (threadIdx.x & 63);
+    const unsigned long long le = __builtin_amdgcn_ballot_w64(i < n && recs[i].*first <= u);
+    at += __builtin_popcountll(le);
+    if (le != ~0ull) break;
+  }
+  return __builtin_amdgcn_readfirstlane(at);
+}
+
+template <typename S, int D, int J, bool KV8>
+__global__ __launch_bounds__(256, J == 1 ? 2 : 1) void attn_step_kernel(FlpStepArgs a, FlpStepList list) {
+  typedef Kind<S, KV8> C;
+  typedef typename C::kvec kvec;
+  typedef typename C::vvec vvec;
+  typedef typename S::storage ST;
+  constexpr int RUN = 16 / C::ES, TP = 4 * RUN, NT = RUN / 4, KC = D * C::ES / 64, CT = D / 16, STEPS = C::STEPS;
+  constexpr int VE = RUN / STEPS;                      // positions of a lane's run that one step of the second product takes
+  __shared__ f32x4 merge_o[4][CT][J][64];
+  __shared__ float2 merge_ml[4][J][16];
+
+  const int lane = threadIdx.x & 63, lr = lane & 15, lh = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int u = blockIdx.x / a.n_kv, g = blockIdx.x - u * a.n_kv;
+  const FlpStepSeq* __restrict__ recs = a.recs ? a.recs : list.seq;
+  const FlpStepSeq rec = recs[find(recs, a.n_recs, u, &FlpStepSeq::unit0)];
+  const int G = a.n_h / a.n_kv, R = rec.n * G, P = rec.prefix, L = P + rec.n;
+  const int rw = a.row_waves, kw = 4 / rw;             // waves side by side on row tiles, and on slices of the context
+  const int groups = (R + 16 * J * rw - 1) / (16 * J * rw);      // workgroups that the rows take
+  const int local = u - rec.unit0, piece = local / groups, rgroup = local - piece * groups;
+  const int row0 = (rgroup * rw + wave % rw) * 16 * J, slice = wave / rw;
+  const bool active = row0 < R;
+  const int row_last = row0 + 16 * J < R ? row0 + 16 * J - 1 : R - 1;
+
+  // tiles of the piece, and those of them that this wave's rows see something of
+  const int n_tiles = (L + TP - 1) / TP;
+  const int lo = (int)((int64_t)n_tiles * piece / rec.pieces);
+  int hi = (int)((int64_t)n_tiles * (piece + 1) / rec.pieces);
+  const int sees = a.mask ? L : P + row_last / G + 1;  // positions that the wave's rows see together
+  if (hi > (sees + TP - 1) / TP) hi = (sees + TP - 1) / TP;
+  const int all_see = a.mask ? P : P + row0 / G + 1;   // positions that each of them sees
+  const float c = a.scale_log2e * (KV8 ? a.k_scale[g] : 1.f);
+
+  // ---- the rows: token and head, the queries, what of the new tokens they see
+  int64_t rowoff[J];
+  int tok[J];
+  uint64_t bits[J];
+  kvec qf[J][KC * STEPS];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int r = row0 + 16 * j + lr, rc = r < R ? r : R - 1;
+    tok[j] = rc / G;
+    rowoff[j] = ((int64_t)(rec.t0 + tok[j]) * a.n_h + (g * G + rc - tok[j] * G)) * D;
+    bits[j] = 0;
+    if (a.mask) bits[j] = a.mask[rec.t0 + tok[j]] & (~0ull >> (64 - rec.n));
+    const ST* qp = reinterpret_cast<const ST*>(a.q) + rowoff[j];
+#pragma unroll
+    for (int cc = 0; cc < KC; ++cc) {
+      constexpr int PER = 16 / C::ES;                  // channels of a lane's 16 bytes of K
+      const ST* p = qp + cc * 4 * PER + lh * PER;
+      if constexpr (std::is_same<S, F32>::value) {
+        const u32x4 raw = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) qf[j][cc * STEPS + s] = __uint_as_float(raw[s]);
+      } else {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) qf[j][cc * STEPS + s] = bits_as<kvec>(*reinterpret_cast<const u32x4*>(p + 8 * s));
+      }
+    }
+  }
+
+  // ---- this lane's place in a tile: its K rows are keys RUN (lr / 4) + 4 t + lr % 4, its run of V starts at position RUN lh
+  const int pb = a.pb, last = (L - 1) / RUN;           // the last run that holds a position of the sequence
+  const int32_t* __restrict__ table = a.tables + (int64_t)rec.seq * a.max_blocks;
+  const int psh = __builtin_ctz(pb);
+  const auto run_of = [&](int tile, int sel) {
+    const int r = 4 * tile + sel;
+    return (r < last ? r : last) * RUN;
+  };
+  const auto id = [&](int tile, int sel) { return table[run_of(tile, sel) >> psh]; };
+  u32x4 kr[NT][KC], vr[CT];
+  const auto load_k = [&](int tile, int32_t blk) {
+    const int slot = (run_of(tile, lr >> 2) & (pb - 1)) + (lr & 3);
+    const uint8_t* p = a.pool + (int64_t)blk * a.block_bytes + ((int64_t)(g * pb + slot) * D) * C::ES + 16 * lh;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int cc = 0; cc < KC; ++cc) kr[t][cc] = *reinterpret_cast<const u32x4*>(p + 4 * t * D * C::ES + 64 * cc);
+  };
+  const auto load_v = [&](int tile, int32_t blk) {
+    const int slot = run_of(tile, lh) & (pb - 1);
+    const uint8_t* p = a.pool + (int64_t)blk * a.block_bytes + ((int64_t)a.n_kv * pb * D + (int64_t)(g * D + lr) * pb + slot) * C::ES;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) vr[ct] = *reinterpret_cast<const u32x4*>(p + (int64_t)16 * ct * pb * C::ES);
+  };
+
+  f32x4 O[CT][J];
+  float m[J], l[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    m[j] = -INFINITY;
+    l[j] = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) O[ct][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // V with values that are not finite: they are replaced by zero, and which sums they would have gone into is kept, a byte per four
+  // channels of a row, in the wave's part of the merge's LDS (bit e of vis: position e of the lane's run).  NaN counts as both infinities.
+  bool flagged = false;
+  uint8_t* const flags = reinterpret_cast<uint8_t*>(&merge_o[wave][0][0][0]) + lane;
+  const auto not_finite = [&](const uint32_t (&vis)[J]) {
+    if (!flagged)
+#pragma unroll 1
+      for (int x = 0; x < CT * J; ++x) flags[64 * x] = 0;
+    flagged = true;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      uint32_t f[J];
+#pragma unroll
+      for (int j = 0; j < J; ++j) f[j] = 0;
+#pragma unroll
+      for (int sign = 0; sign < (KV8 ? 1 : 2); ++sign) {             // e4m3 has no infinities
+        f32x4 n[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) n[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+          const vvec x = C::v(vr[ct], s);
+          vvec is;
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            const float v = got(x, e);
+            put(is, e, v != v || v == (sign ? -INFINITY : INFINITY) ? 1.f : 0.f);
+          }
+#pragma unroll
+          for (int j = 0; j < J; ++j) {
+            vvec seen;
+#pragma unroll
+            for (int e = 0; e < VE; ++e) put(seen, e, (vis[j] >> (VE * s + e)) & 1 ? 1.f : 0.f);
+            n[j] = mma(is, seen, n[j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[j] |= n[j][i] > 0.f ? (KV8 ? 0x11u : sign ? 0x10u : 1u) << i : 0u;
+      }
+#pragma unroll
+      for (int j = 0; j < J; ++j) flags[64 * (ct * J + j)] |= (uint8_t)f[j];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {                    // the high bit of each such value, spread over it
+        const uint32_t o = C::odd(vr[ct][w]);
+        vr[ct][w] &= ~(C::ES == 4 ? 0u - (o >> 31) : C::ES == 2 ? (o >> 15) * 0xffffu : (o >> 7) * 0xffu);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  const auto step = [&](int tile, int next, int32_t next_k, int32_t next_v) {
+    f32x4 s[NT][J];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) s[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int cc = 0; cc < KC; ++cc)
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+          const kvec kv = C::k(kr[t][cc], st);
+#pragma unroll
+          for (int j = 0; j < J; ++j) s[t][j] = mma(kv, qf[j][cc * STEPS + st], s[t][j]);
+        }
+    }
+    if (J == 1) {                                      // on their way during the rest of the step
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(next, next_k);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    const int p0 = TP * tile + RUN * lh;
+    const bool careful = TP * tile + TP > all_see;     // some row does not see the whole tile
+    uint32_t vis[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) vis[j] = (1u << RUN) - 1;
+    if (careful) {
+      const auto low = [&](int n) { return n <= 0 ? 0u : n >= RUN ? (1u << RUN) - 1 : (1u << n) - 1; };
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        if (a.mask) {
+          const int ahead = p0 - P;                    // which new token the run's first position holds
+          const uint64_t b = ahead >= 64 || ahead <= -64 ? 0 : ahead >= 0 ? bits[j] >> ahead : bits[j] << -ahead;
+          vis[j] = low(P - p0) | ((uint32_t)b & ((1u << RUN) - 1));
+        } else {
+          vis[j] = low(P + tok[j] + 1 - p0);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][j][i] = (vis[j] >> (4 * t + i)) & 1 ? s[t][j][i] : -INFINITY;
+      }
+      const uint32_t there = low(L - p0);              // slots past the end hold arbitrary bits
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t keep = 0;
+#pragma unroll
+        for (int e = 0; e < RUN / 4; ++e)
+          if ((there >> (RUN / 4 * w + e)) & 1) keep |= (C::ES == 4 ? 0xffffffffu : C::ES == 2 ? 0xffffu : 0xffu) << (8 * C::ES * e % 32);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) vr[ct][w] &= keep;
+      }
+    }
+    // The running maximum is raised only when a row has outgrown it by 2^8: until then weights are relative to the old one
+    float tm[J];
+    bool grew = false;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      tm[j] = s[0][j][0];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tm[j] = fmaxf(tm[j], s[t][j][i]);
+      grew = grew || (tm[j] - m[j]) * c > 8.f;
+    }
+    if (__builtin_amdgcn_ballot_w64(grew)) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        tm[j] = fmaxf(tm[j], __shfl_xor(tm[j], 16));
+        tm[j] = fmaxf(tm[j], __shfl_xor(tm[j], 32));
+        const float mn = fmaxf(m[j], tm[j]);
+        const float alpha = mn == m[j] ? 1.f : __builtin_amdgcn_exp2f((m[j] - mn) * c);
+        m[j] = mn;
+        l[j] *= alpha;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[ct][j][i] *= alpha;
+      }
+    }
+    vvec w[J][STEPS][C::PIECES];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const float mc = m[j] == -INFINITY ? 0.f : m[j] * c;
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[t][j][i], c, -mc));
+          sum += x;
+          const int e = 4 * t + i;
+          put(w[j][e / VE][0], e % VE, x);
+          if constexpr (C::PIECES == 2) put(w[j][e / VE][1], e % VE, x - got(w[j][e / VE][0], e % VE));
+        }
+      l[j] += sum;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (careful || !KV8) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) any |= C::odd(vr[ct][w]);
+      if (__builtin_amdgcn_ballot_w64(any != 0)) not_finite(vis);
+    }
+    if (J > 1) {                                       // more rows: the scores' registers are free only now
+      load_k(next, next_k);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        const vvec v = C::v(vr[ct], st);
+#pragma unroll
+        for (int pc = C::PIECES - 1; pc >= 0; --pc)
+#pragma unroll
+          for (int j = 0; j < J; ++j) O[ct][j] = mma(v, w[j][st][pc], O[ct][j]);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(next, next_v);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  if (active && lo + slice < hi) {
+    int tile = lo + slice;
+    int32_t idk = id(tile, lr >> 2), idv = id(tile, lh);
+    load_k(tile, idk);
+    load_v(tile, idv);
+    int32_t nk = id(tile + kw, lr >> 2), nv = id(tile + kw, lh);
+    for (; tile < hi; tile += kw) {                    // loads past the end: the last run again, not used
+      idk = nk;
+      idv = nv;
+      nk = id(tile + 2 * kw, lr >> 2);
+      nv = id(tile + 2 * kw, lh);
+      step(tile, tile + kw, idk, idv);
+    }
+  }
+  if (flagged)
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const uint32_t f = flags[64 * (ct * J + j)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if ((f >> i) & 1) O[ct][j][i] += INFINITY;
+          if ((f >> (4 + i)) & 1) O[ct][j][i] -= INFINITY;
+        }
+      }
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    l[j] += __shfl_xor(l[j], 16);
+    l[j] += __shfl_xor(l[j], 32);
+  }
+
+  // ---- slices of the context, then the result or the piece's share of it.  Lane (row lr, quarter lh): channels 16 ct + 4 lh ..
+  const float vs = KV8 ? a.v_scale[g] : 1.f;
+  float M[J], Lsum[J], factor[J][4];
+  if (kw > 1) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (lh == 0) merge_ml[wave][j][lr] = make_float2(m[j], l[j]);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) merge_o[wave][ct][j][lane] = O[ct][j];
+    }
+    __syncthreads();
+  }
+  if (!active) return;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    M[j] = m[j];
+    Lsum[j] = l[j];
+    if (kw > 1) {
+      const int first = wave % rw;
+      float mm[4], ll[4];
+      M[j] = -INFINITY;
+      Lsum[j] = 0.f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float2 v = merge_ml[(first + x * rw) & 3][j][lr];
+        mm[x] = x < kw ? v.x : -INFINITY;
+        ll[x] = v.y;
+        M[j] = fmaxf(M[j], mm[x]);
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        factor[j][x] = mm[x] == -INFINITY ? 0.f : mm[x] == M[j] ? 1.f : __builtin_amdgcn_exp2f((mm[x] - M[j]) * c);
+        if (x < kw) Lsum[j] += factor[j][x] == 0.f ? (ll[x] != ll[x] ? ll[x] : 0.f) : ll[x] * factor[j][x];
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int r = row0 + 16 * j + lr;
+    const bool nothing = a.mask && P == 0 && bits[j] == 0;
+    const float inv = nothing ? 0.f : vs / Lsum[j];
+    const int64_t prow = (int64_t)rec.part0 + (int64_t)tok[j] * rec.pieces + piece;
+    float* const pp = a.partials + (prow * a.n_h + (rowoff[j] / D - (int64_t)(rec.t0 + tok[j]) * a.n_h)) * (D + 2);
+    if (r < R && rec.pieces > 1 && lh == 0 && slice == 0) *reinterpret_cast<float2*>(pp) = make_float2(M[j] * c, Lsum[j]);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      if (kw > 1 && (ct & (kw - 1)) != slice) continue;
+      f32x4 o = O[ct][j];
+      if (kw > 1) {
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int first = wave % rw;
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (x < kw && factor[j][x] != 0.f) {
+            const f32x4 v = merge_o[(first + x * rw) & 3][ct][j][lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], factor[j][x], o[i]);
+          }
+      }
+      if (r >= R) continue;
+      if (rec.pieces > 1) {
+        float2* const d2 = reinterpret_cast<float2*>(pp + 2 + 16 * ct + 4 * lh);
+        d2[0] = make_float2(o[0] * vs, o[1] * vs);
+        d2[1] = make_float2(o[2] * vs, o[3] * vs);
+        continue;
+      }
+      ST* const op = reinterpret_cast<ST*>(a.out) + rowoff[j] + 16 * ct + 4 * lh;
+      ST e[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i] = nothing ? S::from_float(0.f) : S::from_float(o[i] * inv);
+      __builtin_memcpy(__builtin_assume_aligned(op, 4 * sizeof(ST)), e, sizeof(e));
+    }
+  }
+}
+
+// The pieces of a (token, head) row, at most 64, in piece order: a wave per row, lane i piece i's maximum and sum, every lane its channels
+template <typename S, int D>
+__global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, FlpStepList list) {
+  typedef typename S::storage ST;
+  constexpr int CPL = D / 64;
+  typedef float chan __attribute__((ext_vector_type(CPL)));
+  const int lane = threadIdx.x & 63;
+  const int64_t wid = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = (int)(wid / a.n_h), h = (int)(wid - (int64_t)row * a.n_h);
+  if (row >= a.merge_rows) return;
+  const FlpStepSeq* __restrict__ recs = a.recs ? a.recs : list.seq;
+  const FlpStepSeq rec = recs[find(recs, a.n_recs, row, &FlpStepSeq::merge0)];
+  const int tok = row - rec.merge0, ns = rec.pieces;
+  const int64_t stride = (int64_t)a.n_h * (D + 2);
+  const float* __restrict__ pp = a.partials + ((int64_t)rec.part0 + (int64_t)tok * ns) * stride + (int64_t)h * (D + 2);
+  const float* mine = pp + (lane < ns ? lane : 0) * stride;
+  const float mi = mine[0], li = mine[1];
+  constexpr int B = 16;
+  chan q[B];
+  const auto request = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < B; ++i) q[i] = *reinterpret_cast<const chan*>(pp + (int64_t)(i0 + i < ns ? i0 + i : ns - 1) * stride + 2 + CPL * lane);
+  };
+  request(0);
+  float M = lane < ns ? mi : -INFINITY;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
+  // a piece that the row sees nothing of has m = -inf, l = 0
+  const float wi = lane < ns && mi != -INFINITY ? (mi == M ? 1.f : exp2f(mi - M)) : 0.f;
+  float l = lane < ns && (wi != 0.f || li != li) ? (wi != 0.f ? li * wi : li) : 0.f;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) l += __shfl_xor(l, off);
+  float acc[CPL];
+#pragma unroll
+  for (int x = 0; x < CPL; ++x) acc[x] = 0.f;
+  for (int i0 = 0; i0 < ns; i0 += B) {
+    if (i0) request(i0);
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      const float w = __shfl(wi, (i0 + i) & 63);
+      if (i0 + i < ns && w != 0.f)
+#pragma unroll
+        for (int x = 0; x < CPL; ++x) acc[x] = fmaf(q[i][x], w, acc[x]);
+    }
+  }
+  const float inv = 1.f / l;
+  ST* op = reinterpret_cast<ST*>(a.out) + ((int64_t)(rec.t0 + tok) * a.n_h + h) * D + CPL * lane;
+#pragma unroll
+  for (int x = 0; x < CPL; ++x) op[x] = S::from_float(acc[x] * inv);
+}
+
+template <typename S, int D, bool KV8>
+void launch_rows(const FlpStepArgs& a, const FlpStepList& list, int row_tiles, unsigned grid, hipStream_t stream) {
+  if (row_tiles == 1)
+    hipLaunchKernelGGL((attn_step_kernel<S, D, 1, KV8>), dim3(grid), dim3(256), 0, stream, a, list);
+  else if (row_tiles == 2 || std::is_same<S, F32>::value)
+    hipLaunchKernelGGL((attn_step_kernel<S, D, 2, KV8>), dim3(grid), dim3(256), 0, stream, a, list);
+  else if constexpr (!std::is_same<S, F32>::value)
+    hipLaunchKernelGGL((attn_step_kernel<S, D, 4, KV8>), dim3(grid), dim3(256), 0, stream, a, list);
+}
+template <typename S, int D>
+void launch_kind(const FlpStepArgs& a, const FlpStepList& list, int row_tiles, unsigned grid, hipStream_t stream) {
+  if constexpr (!std::is_same<S, F32>::value)
+    if (a.k_scale) return launch_rows<S, D, true>(a, list, row_tiles, grid, stream);
+  launch_rows<S, D, false>(a, list, row_tiles, grid, stream);
+}
+
+}  // namespace
+
+flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles,
+                                int64_t n_units, hipStream_t stream) {
+  if (n_units <= 0) return FLP_OK;
+  const unsigned grid = (unsigned)(n_units * a.n_kv);
+  const bool d64 = head_dim == 64;
+  if (dtype == FLP_F32)
+    d64 ? launch_kind<F32, 64>(a, list, row_tiles, grid, stream) : launch_kind<F32, 128>(a, list, row_tiles, grid, stream);
+  else if (dtype == FLP_F16)
+    d64 ? launch_kind<F16, 64>(a, list, row_tiles, grid, stream) : launch_kind<F16, 128>(a, list, row_tiles, grid, stream);
+  else
+    d64 ? launch_kind<BF16, 64>(a, list, row_tiles, grid, stream) : launch_kind<BF16, 128>(a, list, row_tiles, grid, stream);
+  FLP_TRY_HIP(hipGetLastError());
+  if (a.merge_rows <= 0) return FLP_OK;
+  const dim3 mgrid((unsigned)(((int64_t)a.merge_rows * a.n_h + 3) / 4));
+  const auto merge = [&](auto kernel) { hipLaunchKernelGGL(kernel, mgrid, dim3(256), 0, stream, a, list); };
+  if (dtype == FLP_F32)
+    d64 ? merge(attn_step_merge_kernel<F32, 64>) : merge(attn_step_merge_kernel<F32, 128>);
+  else if (dtype == FLP_F16)
+    d64 ? merge(attn_step_merge_kernel<F16, 64>) : merge(attn_step_merge_kernel<F16, 128>);
+  else
+    d64 ? merge(attn_step_merge_kernel<BF16, 64>) : merge(attn_step_merge_kernel<BF16, 128>);
+  FLP_TRY_HIP(hipGetLastError());
+  return FLP_OK;
+}

@@ -196,6 +196,48 @@ extern "C" int32_t flp_attention_route(int32_t n_q_heads, int32_t n_kv_heads, in
 constexpr int kMfmaRowsPerItem = 256;
 constexpr int kMfmaMaxBlocks = 4096;       // longest context of the matrix-core kernel: 65536 positions
 
+// ---- the 8-bit cache, drafted trees and accepted paths (step.cpp, attention_step.hip, kv8.hip).  The kernels find their work in one
+// record per sequence with new tokens: `unit0` is the first of the launch's workgroup units that belong to it.  Up to
+// kStepInline records travel in the launch's own arguments, more of them through a staging slot.
+struct FlpStepSeq {
+  int32_t seq;                 // row of the block tables
+  int32_t t0, n, prefix;       // first new token, new tokens, positions before them
+  int32_t unit0;
+  int32_t pieces, part0, merge0;   // attention: pieces of the context, first row of the partials, first row of the merge launch
+};
+constexpr int kStepInline = 96;
+struct FlpStepList {
+  FlpStepSeq seq[kStepInline];
+};
+struct FlpStepArgs {
+  uint8_t* pool;
+  int64_t block_bytes;
+  const int32_t* tables;
+  int32_t max_blocks;
+  int32_t n_h, n_kv;
+  int32_t pb;                  // positions per block of this cache: 16, 32 or 64
+  int32_t n_recs, merge_rows;
+  int32_t row_waves;           // attention: waves of a workgroup side by side on row tiles (1, 2 or 4), the others on slices of the context
+  float scale_log2e;
+  const FlpStepSeq* recs;      // null: in the launch's arguments
+  const void* q;
+  void* out;
+  const void* k_new;
+  const void* v_new;
+  const uint64_t* mask;        // trees
+  const float* k_scale;        // 8-bit cache
+  const float* v_scale;
+  float* partials;             // [piece rows][n_h][head_dim + 2] as in FlpAttnArgs
+};
+// row_tiles (1, 2 or 4): tiles of 16 query rows per wave
+flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles,
+                                int64_t n_units, hipStream_t stream);
+constexpr int kAppend8Slots = 32;      // a unit of the 8-bit append: the slots of one such run of positions
+flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int64_t n_units,
+                                 hipStream_t stream);
+flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpStepList& list, const int32_t* n_accept,
+                                const int32_t* path, hipStream_t stream);
+
 struct FlpLoraArgs {
   const uint8_t* pool;
   int64_t block_elems;

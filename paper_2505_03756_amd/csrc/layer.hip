@@ -191,6 +191,93 @@ __global__ __launch_bounds__(256) void rope_kernel(typename S::storage* __restri
   }
 }
 
+// Norms of queries and keys per head and the rotary embedding behind them in one pass: a lane holds 16 bytes of a head's first half
+// and the 16 bytes of the second half that they are paired with, LPH lanes a head, so the sum of squares is a few exchanges
+// between neighbours and a value is rounded once, when it is stored.  One wave takes U x HPW heads of one token; all loads are under way
+// while it computes the token's angles, one per lane: turns in fp64 (position times theta^(-2i/d) / 2 pi, of which only the
+// fraction matters), sine and cosine of the fraction in fp32, shared through the wave's part of LDS.
+struct TurnTable {
+  double per_position[64];     // theta^(-2 i / d) / (2 pi)
+};
+struct QkRows {
+  const void *q_in, *k_in, *w_q, *w_k;
+  void *q_out, *k_out;
+  int64_t ld_q_in, ld_k_in;
+  const int32_t* positions;
+  int32_t T, n_q, n_kv, chunks;    // chunks: waves per token; n_q or n_kv is 0 where that side is not given
+  float eps;
+};
+
+template <typename S, int D, int U>
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRows a, TurnTable turns) {
+  typedef typename S::storage ST;
+  constexpr int N = Vec<S>::N, HALF = D / 2, LPH = HALF / N, HPW = 64 / LPH;
+  __shared__ __attribute__((aligned(16))) float cs[4][HALF], sn[4][HALF];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t item = (int64_t)blockIdx.x * 4 + wave;
+  const int t = (int)(item / a.chunks), chunk = (int)(item - (int64_t)t * a.chunks);
+  if (t >= a.T) return;                                // waves share nothing
+  const int pos = a.positions[t];
+  const int c0 = lane % LPH * N, heads = a.n_q + a.n_kv;
+  Vec<S> x[U][2], w[2][2];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int h = (chunk * U + u) * HPW + lane / LPH;
+    if (h >= heads) break;
+    const ST* p = h < a.n_q ? (const ST*)a.q_in + (int64_t)t * a.ld_q_in + (int64_t)h * D
+                            : (const ST*)a.k_in + (int64_t)t * a.ld_k_in + (int64_t)(h - a.n_q) * D;
+    x[u][0] = ldv<S>(p + c0);
+    x[u][1] = ldv<S>(p + HALF + c0);
+  }
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (a.n_q) w[0][half] = ldv<S>((const ST*)a.w_q + half * HALF + c0);
+    if (a.n_kv) w[1][half] = ldv<S>((const ST*)a.w_k + half * HALF + c0);
+  }
+  if (lane < HALF) {
+    const double turn = (double)pos * turns.per_position[lane];
+    float s, c;
+    sincospif(2.f * (float)(turn - rint(turn)), &s, &c);
+    cs[wave][lane] = c;
+    sn[wave][lane] = s;
+  }
+  __builtin_amdgcn_wave_barrier();
+  float cv[N], sv[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    cv[j] = cs[wave][c0 + j];
+    sv[j] = sn[wave][c0 + j];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int h = (chunk * U + u) * HPW + lane / LPH;
+    if (h >= heads) break;                             // the lanes of a head agree
+    float ss = 0.f;
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float f = S::to_float(x[u][half].e[j]);
+        ss = fmaf(f, f, ss);
+      }
+#pragma unroll
+    for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
+    const float inv = 1.0f / sqrtf(ss / (float)D + a.eps);
+    const bool is_q = h < a.n_q;
+    Vec<S> oa, ob;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float af = S::to_float(x[u][0].e[j]) * inv * S::to_float(is_q ? w[0][0].e[j] : w[1][0].e[j]);
+      const float bf = S::to_float(x[u][1].e[j]) * inv * S::to_float(is_q ? w[0][1].e[j] : w[1][1].e[j]);
+      oa.e[j] = S::from_float(af * cv[j] - bf * sv[j]);
+      ob.e[j] = S::from_float(bf * cv[j] + af * sv[j]);
+    }
+    ST* o = is_q ? (ST*)a.q_out + ((int64_t)t * a.n_q + h) * D : (ST*)a.k_out + ((int64_t)t * a.n_kv + (h - a.n_q)) * D;
+    stv<S>(o + c0, oa);
+    stv<S>(o + HALF + c0, ob);
+  }
+}
+
 template <typename S>
 __global__ __launch_bounds__(256) void silu_mul_kernel(const typename S::storage* __restrict__ gate, int64_t ld_g,
                                                        const typename S::storage* __restrict__ up, int64_t ld_u,
@@ -310,6 +397,55 @@ extern "C" flp_status fll_rope(int32_t dtype, void* q, void* k, const int32_t* p
                                            (S_::storage*)k, positions, n_q_heads, n_kv_heads, l2t));
   FLP_TRY_HIP(hipGetLastError());
   return FLP_OK;
+}
+
+extern "C" flp_status fll_qk_norm_rope(int32_t dtype, const void* q_in, int64_t ld_q_in, const void* k_in, int64_t ld_k_in,
+                                       const void* w_q, const void* w_k, const int32_t* positions, void* q_out, void* k_out,
+                                       int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float eps,
+                                       float theta, void* hip_stream) {
+  if (dtype < FLP_F32 || dtype > FLP_BF16 || n_tokens < 0 || !positions || ((uintptr_t)positions & 3) || !(theta > 0) ||
+      !std::isfinite(theta) || !(eps >= 0) || (q_in && (!w_q || !q_out || n_q_heads <= 0)) ||
+      (k_in && (!w_k || !k_out || n_kv_heads <= 0)) || !aligned16(q_in) || !aligned16(k_in) || !aligned16(w_q) || !aligned16(w_k) ||
+      !aligned16(q_out) || !aligned16(k_out)) {
+    flp_set_error("fll_qk_norm_rope: bad dtype / sizes / eps / theta or null / misaligned pointer");
+    return FLP_EINVAL;
+  }
+  if (head_dim != 64 && head_dim != 128) {
+    flp_set_error("fll_qk_norm_rope: head_dim %d not supported (64 or 128)", head_dim);
+    return FLP_ENOTSUP;
+  }
+  if ((q_in && ld_q_in < (int64_t)n_q_heads * head_dim) || (k_in && ld_k_in < (int64_t)n_kv_heads * head_dim)) {
+    flp_set_error("fll_qk_norm_rope: a leading dimension is smaller than a row");
+    return FLP_EINVAL;
+  }
+  const int eb = elem_bytes(dtype);
+  if ((q_in && ld_q_in * eb % 16) || (k_in && ld_k_in * eb % 16)) {
+    flp_set_error("fll_qk_norm_rope: leading dimensions must be multiples of 16 bytes");
+    return FLP_ENOTSUP;
+  }
+  if (n_tokens == 0 || (!q_in && !k_in)) return FLP_OK;
+  QkRows a{q_in, k_in, w_q, w_k, q_out, k_out, ld_q_in, ld_k_in, positions, n_tokens, q_in ? n_q_heads : 0, k_in ? n_kv_heads : 0, 0, eps};
+  TurnTable turns{};
+  for (int i = 0; i < head_dim / 2; ++i)
+    turns.per_position[i] = std::exp2(-2.0 * i / head_dim * std::log2((double)theta)) / 6.283185307179586476925287;
+  const int per_wave = 64 / (head_dim / 2 / (16 / eb)), groups = (a.n_q + a.n_kv + per_wave - 1) / per_wave;
+  const auto launch = [&](auto unroll) -> flp_status {
+    constexpr int U = decltype(unroll)::value;
+    a.chunks = (groups + U - 1) / U;
+    const int64_t blocks = ((int64_t)n_tokens * a.chunks + 3) / 4;
+    if (blocks > INT32_MAX) {
+      flp_set_error("fll_qk_norm_rope: more heads than one launch takes");
+      return FLP_ERANGE;
+    }
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (head_dim == 64)
+      FLL_BY_DTYPE(dtype, hipLaunchKernelGGL((qk_norm_rope_kernel<S_, 64, U>), dim3((unsigned)blocks), dim3(256), 0, st, a, turns));
+    else
+      FLL_BY_DTYPE(dtype, hipLaunchKernelGGL((qk_norm_rope_kernel<S_, 128, U>), dim3((unsigned)blocks), dim3(256), 0, st, a, turns));
+    FLP_TRY_HIP(hipGetLastError());
+    return FLP_OK;
+  };
+  return launch(std::integral_constant<int, 1>{});
 }
 
 extern "C" flp_status fll_silu_mul(int32_t dtype, const void* gate, int64_t ld_gate, const void* up, int64_t ld_up,

@@ -1,0 +1,366 @@
+// Host side of the calls over an 8-bit cache, of drafted trees and of accepted paths: argument checks, the records of the
+// sequences, and the launches.  C ABI in flpool.h, kernels in attention_step.hip and kv8.hip.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "flp_internal.h"
+
+namespace {
+
+bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+// e4m3 positions in a block's bytes
+int kv8_tokens(const flp_pool* p) { return p->elem_bytes == 2 ? 2 * p->cfg.block_tokens : 0; }
+
+flp_status check_device(const flp_pool* p, const char* who) {
+  int cur = -1;
+  FLP_TRY_HIP(hipGetDevice(&cur));
+  if (cur != p->device) {
+    flp_set_error("%s: device %d is current, the pool lives on device %d", who, cur, p->device);
+    return FLP_EINVAL;
+  }
+  return FLP_OK;
+}
+
+struct Call {
+  const char* who;
+  bool kv8, need_qo, need_kv;
+  int32_t most_new;            // new tokens that a sequence may have; 0: any number
+};
+
+// The checks of a batch; `recs`: the sequences with new tokens, unit0 and what follows still to be filled in
+flp_status check_batch(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, const Call& c, std::vector<FlpStepSeq>* recs) {
+  if (!p || !b) {
+    flp_set_error("%s: null pool or batch", c.who);
+    return FLP_EINVAL;
+  }
+  if (b->n_seqs < 0 || b->max_blocks_per_seq < 0 || (b->n_seqs > 0 && (!b->cu_new || !b->prefix_len || !b->block_tables)) ||
+      !aligned(b->block_tables, 4)) {
+    flp_set_error("%s: bad sequence arrays", c.who);
+    return FLP_EINVAL;
+  }
+  if ((p->cfg.block_tokens != 16 && p->cfg.block_tokens != 32) || (p->cfg.head_dim != 64 && p->cfg.head_dim != 128)) {
+    flp_set_error("%s: kernels support block_tokens 16 or 32 and head_dim 64/128 (pool has %d / %d)", c.who, p->cfg.block_tokens,
+                  p->cfg.head_dim);
+    return FLP_ENOTSUP;
+  }
+  if (c.kv8 && !kv8_tokens(p)) {
+    flp_set_error("%s: an fp32 pool holds no 8-bit cache", c.who);
+    return FLP_ENOTSUP;
+  }
+  if (sc && (!sc->k_scale || !sc->v_scale || !aligned(sc->k_scale, 4) || !aligned(sc->v_scale, 4))) {
+    flp_set_error("%s: null or misaligned scales", c.who);
+    return FLP_EINVAL;
+  }
+  if (c.need_qo && (b->n_q_heads <= 0 || b->n_q_heads % p->cfg.n_kv_heads)) {
+    flp_set_error("%s: n_q_heads %d is not a multiple of n_kv_heads %d", c.who, b->n_q_heads, p->cfg.n_kv_heads);
+    return FLP_EINVAL;
+  }
+  if (b->n_seqs > 0 && b->cu_new[0] != 0) {
+    flp_set_error("%s: cu_new[0] must be 0", c.who);
+    return FLP_EINVAL;
+  }
+  const int64_t cap = (int64_t)b->max_blocks_per_seq * (c.kv8 ? kv8_tokens(p) : p->cfg.block_tokens);
+  for (int32_t i = 0; i < b->n_seqs; ++i) {
+    const int64_t n = (int64_t)b->cu_new[i + 1] - b->cu_new[i];
+    if (n < 0 || b->prefix_len[i] < 0) {
+      flp_set_error("%s: sequence %d has negative length", c.who, i);
+      return FLP_EINVAL;
+    }
+    if (b->prefix_len[i] + n > cap || b->prefix_len[i] + n > INT32_MAX - 4096) {
+      flp_set_error("%s: sequence %d needs %lld positions, its block table covers %lld", c.who, i,
+                    (long long)(b->prefix_len[i] + n), (long long)cap);
+      return FLP_ERANGE;
+    }
+    if (c.most_new && n > c.most_new) {
+      flp_set_error("%s: sequence %d has %lld new tokens, at most %d supported", c.who, i, (long long)n, c.most_new);
+      return FLP_ERANGE;
+    }
+    if (n > 0) recs->push_back(FlpStepSeq{i, b->cu_new[i], (int32_t)n, b->prefix_len[i], 0, 1, 0, 0});
+  }
+  if (recs->empty()) return FLP_OK;
+  if (c.need_qo && (!b->q || !b->out || !aligned(b->q, 16) || !aligned(b->out, 16))) {
+    flp_set_error("%s: q/out must be non-null and 16-byte aligned", c.who);
+    return FLP_EINVAL;
+  }
+  if (c.need_kv && (!b->k_new || !b->v_new || !aligned(b->k_new, 16) || !aligned(b->v_new, 16))) {
+    flp_set_error("%s: k_new/v_new must be non-null and 16-byte aligned", c.who);
+    return FLP_EINVAL;
+  }
+  return FLP_OK;
+}
+
+FlpStepArgs make_args(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, bool kv8) {
+  FlpStepArgs a{};
+  a.pool = p->dev_base;
+  a.block_bytes = p->block_bytes;
+  a.tables = b->block_tables;
+  a.max_blocks = b->max_blocks_per_seq;
+  a.n_h = b->n_q_heads;
+  a.n_kv = p->cfg.n_kv_heads;
+  a.pb = kv8 ? kv8_tokens(p) : p->cfg.block_tokens;
+  a.row_waves = 1;
+  a.q = b->q;
+  a.out = b->out;
+  a.k_new = b->k_new;
+  a.v_new = b->v_new;
+  if (sc) {
+    a.k_scale = sc->k_scale;
+    a.v_scale = sc->v_scale;
+  }
+  a.scale_log2e = (b->sm_scale > 0.f ? b->sm_scale : 1.0f / std::sqrt((float)p->cfg.head_dim)) * 1.4426950408889634f;
+  return a;
+}
+
+// Where a launch finds its records: in its own arguments, or behind them in one staging slot of the call
+struct Staged {
+  FlpStageSlot* slot = nullptr;
+  size_t used = 0;
+};
+
+bool inline_records(const std::vector<FlpStepSeq>& recs) { return recs.size() <= (size_t)kStepInline; }
+
+// Staging slots and the workspace are handed from call to call by events, which a replayed graph would not see
+flp_status refuse_capture(hipStream_t stream, const char* who) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  FLP_TRY_HIP(hipStreamIsCapturing(stream, &st));
+  if (st != hipStreamCaptureStatusNone) {
+    flp_set_error("%s: this batch needs a staging slot or the pool's workspace and cannot be captured", who);
+    return FLP_ENOTSUP;
+  }
+  return FLP_OK;
+}
+
+// The records of one launch, in `list` or at the next place of the slot
+void place(Staged& st, const std::vector<FlpStepSeq>& recs, FlpStepArgs* a, FlpStepList* list) {
+  a->n_recs = (int32_t)recs.size();
+  const size_t bytes = recs.size() * sizeof(FlpStepSeq);
+  if (inline_records(recs)) {
+    memcpy(list->seq, recs.data(), bytes);
+    return;
+  }
+  memcpy((uint8_t*)st.slot->host + st.used, recs.data(), bytes);
+  a->recs = (const FlpStepSeq*)((const uint8_t*)st.slot->dev + st.used);
+  st.used += bytes;
+}
+
+// units of the append: the runs of kAppend8Slots positions that get new slots
+int64_t append_plan(std::vector<FlpStepSeq>& recs) {
+  int64_t n = 0;
+  for (FlpStepSeq& r : recs) {
+    r.unit0 = (int32_t)n;
+    n += (r.prefix + r.n - 1) / kAppend8Slots - r.prefix / kAppend8Slots + 1;
+  }
+  return n;
+}
+
+// One launch of the attention kernel
+struct AttnLaunch {
+  std::vector<FlpStepSeq> recs;
+  int32_t row_tiles, row_waves, merge_rows;
+  int64_t units;
+};
+
+// Sequences with up to 64 query rows per kv head go in one launch, those with more in another: the first has a wave take all rows and the
+// workgroup's four waves a slice of the context each, the second has the waves share K and V between row tiles.
+// Contexts are cut into pieces of equal length, at least kMinPiece tiles for every wave, so that a launch has about kUnits workgroups.
+constexpr int64_t kUnits = 1024;
+constexpr int kMinPiece = 4, kMaxPieces = 64;
+constexpr int kFewRows = 64;
+
+std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, const std::vector<FlpStepSeq>& all, size_t* part_rows) {
+  std::vector<AttnLaunch> launches;
+  const int tile = 64 / elem_bytes, n_kv = p->cfg.n_kv_heads;
+  int64_t parts = 0;
+  for (int many = 1; many >= 0; --many) {
+    AttnLaunch l{};
+    int64_t rows = 0;
+    for (const FlpStepSeq& r : all)
+      if (((int64_t)r.n * G > kFewRows) == (many == 1)) {
+        l.recs.push_back(r);
+        rows = std::max<int64_t>(rows, (int64_t)r.n * G);
+      }
+    if (l.recs.empty()) continue;
+    l.row_tiles = rows <= 16 ? 1 : rows <= 32 || elem_bytes == 4 ? 2 : 4;      // fp32: four tiles do not fit the registers
+    l.row_waves = rows <= 16 * l.row_tiles ? 1 : rows <= 32 * l.row_tiles ? 2 : 4;
+    const int per_group = 16 * l.row_tiles * l.row_waves;
+    const auto tiles = [&](const FlpStepSeq& r) { return ((int64_t)r.prefix + r.n + tile - 1) / tile; };
+    const auto groups = [&](const FlpStepSeq& r) { return ((int64_t)r.n * G + per_group - 1) / per_group; };
+    std::stable_sort(l.recs.begin(), l.recs.end(), [&](const FlpStepSeq& x, const FlpStepSeq& y) { return tiles(x) > tiles(y); });
+    int64_t total = 0;
+    for (const FlpStepSeq& r : l.recs) total += groups(r) * tiles(r) * n_kv;
+    const int64_t piece = std::max<int64_t>(kMinPiece * (4 / l.row_waves), (total + kUnits - 1) / kUnits);
+    for (FlpStepSeq& r : l.recs) {
+      r.pieces = (int32_t)std::min<int64_t>(kMaxPieces, (tiles(r) + piece - 1) / piece);
+      r.unit0 = (int32_t)l.units;
+      l.units += groups(r) * r.pieces;
+      r.part0 = (int32_t)parts;
+      r.merge0 = l.merge_rows;
+      if (r.pieces > 1) {
+        parts += (int64_t)r.n * r.pieces;
+        l.merge_rows += r.n;
+      }
+    }
+    launches.push_back(std::move(l));
+  }
+  *part_rows = (size_t)parts;
+  return launches;
+}
+
+// An append, an attention, or both in this order, of a batch that has passed the checks
+flp_status run(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, const uint64_t* mask, bool append8, bool attend,
+               const std::vector<FlpStepSeq>& recs, hipStream_t stream, const char* who) {
+  std::lock_guard<std::mutex> lk(p->mu);
+  std::vector<FlpStepSeq> add;
+  int64_t add_units = 0;
+  if (append8) {
+    add = recs;
+    add_units = append_plan(add);
+  }
+  std::vector<AttnLaunch> launches;
+  size_t part_rows = 0;
+  if (attend) launches = attn_plan(p, b->n_q_heads / p->cfg.n_kv_heads, sc ? 1 : p->elem_bytes, recs, &part_rows);
+  for (const AttnLaunch& l : launches)
+    if (l.units * p->cfg.n_kv_heads > INT32_MAX || (int64_t)l.merge_rows * b->n_q_heads > INT32_MAX) {
+      flp_set_error("%s: more rows than one launch takes", who);
+      return FLP_ERANGE;
+    }
+  size_t staged = inline_records(add) ? 0 : add.size();
+  for (const AttnLaunch& l : launches) staged += inline_records(l.recs) ? 0 : l.recs.size();
+  Staged st;
+  float* partials = nullptr;
+  if (staged || part_rows) {
+    FLP_TRY(refuse_capture(stream, who));
+    if (part_rows) {
+      void* w = nullptr;
+      FLP_TRY(flp_attn_workspace(p, part_rows * b->n_q_heads * (p->cfg.head_dim + 2) * sizeof(float), stream, &w));
+      partials = (float*)w;
+    }
+    FLP_TRY(flp_stage_acquire(p, staged * sizeof(FlpStepSeq), &st.slot));
+  }
+  // every launch's records first, then one upload of what is staged
+  FlpStepArgs base = make_args(p, b, sc, sc != nullptr), add_args = base;
+  base.mask = mask;
+  base.partials = partials;
+  FlpStepList lists[3];
+  std::vector<FlpStepArgs> args;
+  if (append8) place(st, add, &add_args, &lists[2]);
+  for (const AttnLaunch& l : launches) {
+    FlpStepArgs a = base;
+    a.merge_rows = l.merge_rows;
+    a.row_waves = l.row_waves;
+    place(st, l.recs, &a, &lists[args.size()]);
+    args.push_back(a);
+  }
+  flp_status s = staged ? flp_stage_upload(st.slot, st.used, stream) : FLP_OK;
+  if (s == FLP_OK && append8) s = flp_launch_kv_append8(p->cfg.dtype, p->cfg.head_dim, add_args, lists[2], add_units, stream);
+  for (size_t i = 0; i < launches.size() && s == FLP_OK; ++i)
+    s = flp_launch_attn_step(p->cfg.dtype, p->cfg.head_dim, args[i], lists[i], launches[i].row_tiles, launches[i].units, stream);
+  if (!st.slot) return s;
+  const flp_status released = flp_stage_release(st.slot, stream);
+  if (part_rows && released == FLP_OK) {
+    p->attn_slot = st.slot;
+    p->attn_stream = stream;
+  }
+  return s != FLP_OK ? s : released;
+}
+
+// no exception leaves the C ABI: the lists are the only allocations
+template <typename F>
+flp_status guarded(const char* who, F f) {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    flp_set_error("%s: out of host memory", who);
+    return FLP_ENOSPC;
+  }
+}
+
+}  // namespace
+
+extern "C" int64_t flp_pool_kv8_block_tokens(const flp_pool* p) { return p ? kv8_tokens(p) : 0; }
+
+extern "C" flp_status flp_kv_append8(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, void* hip_stream) {
+  static const char who[] = "flp_kv_append8";
+  return guarded(who, [&]() -> flp_status {
+    std::vector<FlpStepSeq> recs;
+    if (!sc) {
+      flp_set_error("%s: null scales", who);
+      return FLP_EINVAL;
+    }
+    FLP_TRY(check_batch(p, b, sc, Call{who, true, false, true, 0}, &recs));
+    if (recs.empty()) return FLP_OK;
+    FLP_TRY(check_device(p, who));
+    return run(p, b, sc, nullptr, true, false, recs, (hipStream_t)hip_stream, who);
+  });
+}
+
+extern "C" flp_status flp_paged_prefix_attention8(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, void* hip_stream) {
+  static const char who[] = "flp_paged_prefix_attention8";
+  return guarded(who, [&]() -> flp_status {
+    std::vector<FlpStepSeq> recs;
+    if (!sc) {
+      flp_set_error("%s: null scales", who);
+      return FLP_EINVAL;
+    }
+    const bool append = b && (b->k_new || b->v_new);
+    FLP_TRY(check_batch(p, b, sc, Call{who, true, true, append, 0}, &recs));
+    if (recs.empty()) return FLP_OK;
+    FLP_TRY(check_device(p, who));
+    return run(p, b, sc, nullptr, append, true, recs, (hipStream_t)hip_stream, who);
+  });
+}
+
+extern "C" flp_status flp_paged_tree_attention(flp_pool* p, const flp_attn_batch* b, const uint64_t* tree_mask,
+                                               const flp_kv8_scales* sc, void* hip_stream) {
+  static const char who[] = "flp_paged_tree_attention";
+  return guarded(who, [&]() -> flp_status {
+    std::vector<FlpStepSeq> recs;
+    const bool append = b && (b->k_new || b->v_new);
+    FLP_TRY(check_batch(p, b, sc, Call{who, sc != nullptr, true, append, 64}, &recs));
+    if (recs.empty()) return FLP_OK;
+    if (!tree_mask || !aligned(tree_mask, 8)) {
+      flp_set_error("%s: null or misaligned tree_mask", who);
+      return FLP_EINVAL;
+    }
+    FLP_TRY(check_device(p, who));
+    if (append && !sc) {                               // the pool's own append, whose units are staged
+      FLP_TRY(refuse_capture((hipStream_t)hip_stream, who));
+      FLP_TRY(flp_kv_append(p, b, hip_stream));
+    }
+    return run(p, b, sc, tree_mask, append && sc, true, recs, (hipStream_t)hip_stream, who);
+  });
+}
+
+extern "C" flp_status flp_kv_accept(flp_pool* p, const flp_attn_batch* b, const int32_t* n_accept, const int32_t* path, int32_t kv8,
+                                    void* hip_stream) {
+  static const char who[] = "flp_kv_accept";
+  return guarded(who, [&]() -> flp_status {
+    std::vector<FlpStepSeq> recs;
+    if (kv8 != 0 && kv8 != 1) {
+      flp_set_error("%s: kv8 must be 0 or 1", who);
+      return FLP_EINVAL;
+    }
+    FLP_TRY(check_batch(p, b, nullptr, Call{who, kv8 == 1, false, false, 0}, &recs));
+    if (recs.empty()) return FLP_OK;
+    if (!n_accept || !path || !aligned(n_accept, 4) || !aligned(path, 4)) {
+      flp_set_error("%s: null or misaligned n_accept / path", who);
+      return FLP_EINVAL;
+    }
+    FLP_TRY(check_device(p, who));
+    hipStream_t stream = (hipStream_t)hip_stream;
+    const FlpStepArgs a0 = make_args(p, b, nullptr, kv8 == 1);
+    // sequences are independent: as many launches as the arguments' records take
+    for (size_t i = 0; i < recs.size(); i += kStepInline) {
+      FlpStepArgs a = a0;
+      FlpStepList list;
+      a.n_recs = (int32_t)std::min<size_t>(kStepInline, recs.size() - i);
+      memcpy(list.seq, recs.data() + i, a.n_recs * sizeof(FlpStepSeq));
+      FLP_TRY(flp_launch_kv_accept(kv8 ? 1 : p->elem_bytes, p->cfg.head_dim, a, list, n_accept, path, stream));
+    }
+    return FLP_OK;
+  });
+}

@@ -9,7 +9,7 @@ import numpy as np
 from . import flpool
 from .flpool import _check, _ptr, _stream
 
-EXPORTS = ("fll_rmsnorm", "fll_add_rmsnorm", "fll_rope", "fll_silu_mul", "fll_layer_scratch_bytes",
+EXPORTS = ("fll_rmsnorm", "fll_add_rmsnorm", "fll_rope", "fll_qk_norm_rope", "fll_silu_mul", "fll_layer_scratch_bytes",
            "fll_layer_forward")
 PROJ_ORDER = ("q", "k", "v", "o", "gate", "up", "down")
 
@@ -48,6 +48,7 @@ def _lib():
         L.fll_rmsnorm.argtypes = [i32, vp, vp, vp, i32, i32, f32, vp]
         L.fll_add_rmsnorm.argtypes = [i32, vp, vp, vp, vp, i32, i32, f32, vp]
         L.fll_rope.argtypes = [i32, vp, vp, vp, i32, i32, i32, i32, f32, vp]
+        L.fll_qk_norm_rope.argtypes = [i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, f32, f32, vp]
         L.fll_silu_mul.argtypes = [i32, vp, i64, vp, i64, vp, i64, i32, i32, vp]
         L.fll_layer_scratch_bytes.argtypes = [vp, C.POINTER(LayerConfig), i32]
         L.fll_layer_scratch_bytes.restype = i64
@@ -73,6 +74,13 @@ def add_rmsnorm(dtype, resid, delta, w, y, n_tokens, hidden, eps=1e-5, stream=No
 def rope(dtype, q, k, positions, n_tokens, n_q_heads, n_kv_heads, head_dim, theta=10000.0, stream=None):
     _check(_lib().fll_rope(_dt(dtype), _ptr(q), _ptr(k), _ptr(positions), n_tokens, n_q_heads, n_kv_heads, head_dim,
                            theta, _stream(stream)))
+
+
+def qk_norm_rope(dtype, q_in, k_in, w_q, w_k, positions, q_out, k_out, n_tokens, n_q_heads, n_kv_heads, head_dim, eps=1e-5,
+                 theta=10000.0, ld_q_in=None, ld_k_in=None, stream=None):
+    _check(_lib().fll_qk_norm_rope(_dt(dtype), _ptr(q_in), ld_q_in or n_q_heads * head_dim, _ptr(k_in),
+                                   ld_k_in or n_kv_heads * head_dim, _ptr(w_q), _ptr(w_k), _ptr(positions), _ptr(q_out),
+                                   _ptr(k_out), n_tokens, n_q_heads, n_kv_heads, head_dim, eps, theta, _stream(stream)))
 
 
 def silu_mul(dtype, gate, up, out, n_tokens, width, ld_gate=None, ld_up=None, ld_out=None, stream=None):

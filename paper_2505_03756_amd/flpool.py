@@ -26,7 +26,8 @@ MAX_PROJ = 4
 EXPORTS = ("flp_pool_create", "flp_pool_destroy", "flp_pool_block_bytes", "flp_pool_num_free", "flp_pool_base",
            "flp_pool_alloc", "flp_pool_free", "flp_pool_swap_in", "flp_pool_swap_out", "flp_kv_append",
            "flp_paged_prefix_attention", "flp_lora_apply_paged", "flp_lora_segment", "flp_last_error",
-           "flp_version", "flp_lora_apply_paged_static", "flp_static_scratch_bytes")
+           "flp_version", "flp_lora_apply_paged_static", "flp_static_scratch_bytes", "flp_pool_kv8_block_tokens",
+           "flp_kv_append8", "flp_paged_prefix_attention8", "flp_paged_tree_attention", "flp_kv_accept")
 
 
 class FlpError(RuntimeError):
@@ -46,6 +47,10 @@ class AttnBatch(C.Structure):
                 ("sm_scale", C.c_float), ("q", C.c_void_p), ("k_new", C.c_void_p), ("v_new", C.c_void_p),
                 ("out", C.c_void_p), ("cu_new", C.c_void_p), ("prefix_len", C.c_void_p),
                 ("block_tables", C.c_void_p)]
+
+
+class Kv8Scales(C.Structure):
+    _fields_ = [("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
 class LoraProj(C.Structure):
@@ -99,6 +104,12 @@ def load():
     lib.flp_lora_segment.argtypes = [vp, i32, vp, i32, vp, vp, vp, vp, vp]
     lib.flp_lora_apply_paged_static.argtypes = [vp, C.POINTER(LoraBatch), vp]
     lib.flp_static_scratch_bytes.restype = i64
+    lib.flp_pool_kv8_block_tokens.argtypes = [vp]
+    lib.flp_pool_kv8_block_tokens.restype = i64
+    lib.flp_kv_append8.argtypes = [vp, C.POINTER(AttnBatch), C.POINTER(Kv8Scales), vp]
+    lib.flp_paged_prefix_attention8.argtypes = [vp, C.POINTER(AttnBatch), C.POINTER(Kv8Scales), vp]
+    lib.flp_paged_tree_attention.argtypes = [vp, C.POINTER(AttnBatch), vp, C.POINTER(Kv8Scales), vp]
+    lib.flp_kv_accept.argtypes = [vp, C.POINTER(AttnBatch), vp, vp, i32, vp]
     lib.flp_last_error.restype = C.c_char_p
     lib.flp_version.restype = C.c_char_p
     for name in EXPORTS:
@@ -215,6 +226,40 @@ class Pool:
         mb = block_tables.shape[1] if max_blocks is None else max_blocks
         b, keep = self._attn_batch(cu_new, prefix_len, block_tables, mb, n_q_heads, q, out, k_new, v_new, sm_scale)
         _check(self._lib.flp_paged_prefix_attention(self._h, C.byref(b), _stream(stream)))
+
+    # ---- the 8-bit cache, drafted trees, accepted paths
+    @property
+    def kv8_block_tokens(self):
+        """Positions per block that holds K and V in 8 bits (0: fp32 pools hold none)."""
+        return int(self._lib.flp_pool_kv8_block_tokens(self._h))
+
+    def kv_append8(self, k_new, v_new, k_scale, v_scale, cu_new, prefix_len, block_tables, max_blocks=None, stream=None):
+        mb = block_tables.shape[1] if max_blocks is None else max_blocks
+        b, keep = self._attn_batch(cu_new, prefix_len, block_tables, mb, 0, None, None, k_new, v_new, 0.0)
+        sc = Kv8Scales(_ptr(k_scale), _ptr(v_scale))
+        _check(self._lib.flp_kv_append8(self._h, C.byref(b), C.byref(sc), _stream(stream)))
+
+    def paged_prefix_attention8(self, q, out, k_scale, v_scale, cu_new, prefix_len, block_tables, n_q_heads, k_new=None,
+                                v_new=None, sm_scale=0.0, max_blocks=None, stream=None):
+        mb = block_tables.shape[1] if max_blocks is None else max_blocks
+        b, keep = self._attn_batch(cu_new, prefix_len, block_tables, mb, n_q_heads, q, out, k_new, v_new, sm_scale)
+        sc = Kv8Scales(_ptr(k_scale), _ptr(v_scale))
+        _check(self._lib.flp_paged_prefix_attention8(self._h, C.byref(b), C.byref(sc), _stream(stream)))
+
+    def paged_tree_attention(self, q, out, tree_mask, cu_new, prefix_len, block_tables, n_q_heads, k_new=None, v_new=None,
+                             k_scale=None, v_scale=None, sm_scale=0.0, max_blocks=None, stream=None):
+        """tree_mask: device uint64 (or int64) [T], bit j: the token sees new token j of its sequence.  With k_scale and v_scale
+        the cache is the one of kv_append8, without them it has the pool's type."""
+        mb = block_tables.shape[1] if max_blocks is None else max_blocks
+        b, keep = self._attn_batch(cu_new, prefix_len, block_tables, mb, n_q_heads, q, out, k_new, v_new, sm_scale)
+        sc = None if k_scale is None and v_scale is None else C.byref(Kv8Scales(_ptr(k_scale), _ptr(v_scale)))
+        _check(self._lib.flp_paged_tree_attention(self._h, C.byref(b), _ptr(tree_mask), sc, _stream(stream)))
+
+    def kv_accept(self, n_accept, path, cu_new, prefix_len, block_tables, kv8=False, max_blocks=None, stream=None):
+        """n_accept: device int32 [n_seqs]; path: device int32 [T], the accepted tokens of sequence i from cu_new[i] on."""
+        mb = block_tables.shape[1] if max_blocks is None else max_blocks
+        b, keep = self._attn_batch(cu_new, prefix_len, block_tables, mb, 0, None, None, None, None, 0.0)
+        _check(self._lib.flp_kv_accept(self._h, C.byref(b), _ptr(n_accept), _ptr(path), int(kv8), _stream(stream)))
 
     # ---- a3 / a4 / a5
     def lora_segment(self, token_adapter, n_tokens, n_adapters, n_seg, seg_adapter, seg_start, perm, stream=None):
