@@ -196,14 +196,22 @@ extern "C" int32_t flp_attention_route(int32_t n_q_heads, int32_t n_kv_heads, in
 constexpr int kMfmaRowsPerItem = 256;
 constexpr int kMfmaMaxBlocks = 4096;       // longest context of the matrix-core kernel: 65536 positions
 
-// ---- the 8-bit cache, drafted trees and accepted paths (step.cpp, attention_step.hip, kv8.hip).  The kernels find their work in one
-// record per sequence with new tokens: `unit0` is the first of the launch's workgroup units that belong to it.  Up to
-// kStepInline records travel in the launch's own arguments, more of them through a staging slot.
+// ---- the 8-bit cache, drafted trees and accepted paths (step.cpp, attention_step.hip, kv8.hip)
+// The append and the accept launches find their sequences in their own arguments: sequences seq0 .. seq0 + n - 1 of the batch, the new
+// tokens t0[i] .. t0[i + 1] - 1 each, unit0[i]: the first of the append's units that belong to it.  A batch of more takes
+// several launches.
+constexpr int kListSeqs = 300;
+struct FlpSeqList {
+  int32_t seq0, n;
+  int32_t t0[kListSeqs + 1], prefix[kListSeqs], unit0[kListSeqs];
+};
+// The attention launches have one record per sequence with new tokens: `unit0` is the first of the launch's workgroup units that
+// belong to it.  Up to kStepInline records travel in the launch's own arguments, more of them through a staging slot.
 struct FlpStepSeq {
   int32_t seq;                 // row of the block tables
   int32_t t0, n, prefix;       // first new token, new tokens, positions before them
   int32_t unit0;
-  int32_t pieces, part0, merge0;   // attention: pieces of the context, first row of the partials, first row of the merge launch
+  int32_t pieces, part0, merge0;   // pieces of the context, first row of the partials, first row of the merge launch
 };
 constexpr int kStepInline = 96;
 struct FlpStepList {
@@ -233,9 +241,9 @@ struct FlpStepArgs {
 flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles,
                                 int64_t n_units, hipStream_t stream);
 constexpr int kAppend8Slots = 32;      // a unit of the 8-bit append: the slots of one such run of positions
-flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int64_t n_units,
+flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, int32_t n_units,
                                  hipStream_t stream);
-flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpStepList& list, const int32_t* n_accept,
+flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, const int32_t* n_accept,
                                 const int32_t* path, hipStream_t stream);
 
 struct FlpLoraArgs {

@@ -19,79 +19,116 @@ __device__ __forceinline__ float quotient(float x, float s, float r) {
   return x != x ? x : copysignf(q, x);
 }
 
-// One workgroup per (run of 32 slots, 1024 elements of a token's row) unit; a thread owns 4 channels of one head.  K: the threads'
-// words of a token are contiguous.  V: a thread turns its channels' 32 slots into their 32-byte runs of the transposed V, whole
-// sectors; with runs of 16 slots per unit every sector would be written by two workgroups.  A unit that covers part of its run (the ends
-// of a sequence's new tokens, single tokens) writes whole words where all four slots are new and single bytes elsewhere.
+// Workgroups of K and workgroups of V per unit of 32 slots and 1024 elements of a token's row; all reads of a thread are on their
+// way together.  K: a thread owns 8 channels of 16 slots.  V: a thread owns 4 channels and turns their 32 slots into their 32-byte runs of
+// the transposed V, whole sectors.  A unit that covers part of its run (the ends of a sequence's new tokens) merges its slots into the
+// 16-byte words already there, which belong to this sequence alone; units of one or two slots (a decode batch) store single bytes.
 template <typename S, int D>
-__global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpStepList list) {
+__global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqList list) {
   typedef typename S::storage ST;
-  constexpr int SL = kAppend8Slots, C = 4;
-  const int row = a.n_kv * D;
-  const int e0 = (blockIdx.y * 256 + threadIdx.x) * C;
-  const int u = blockIdx.x;
-  const FlpStepSeq* __restrict__ recs = a.recs ? a.recs : list.seq;
-  int at = -1;
-  for (int base = 0; base < a.n_recs; base += 64) {
+  constexpr int SL = kAppend8Slots;
+  const int row = a.n_kv * D, u = blockIdx.x;
+  const bool is_v = blockIdx.y & 1;
+  int rec = -1;                                        // the last sequence whose first unit is not behind u
+  for (int base = 0; base < list.n; base += 64) {
     const int i = base + (threadIdx.x & 63);
-    const unsigned long long le = __builtin_amdgcn_ballot_w64(i < a.n_recs && recs[i].unit0 <= u);
-    at += __builtin_popcountll(le);
+    const unsigned long long le = __builtin_amdgcn_ballot_w64(i < list.n && list.unit0[i] <= u);
+    rec += __builtin_popcountll(le);
     if (le != ~0ull) break;
   }
-  const FlpStepSeq rec = recs[__builtin_amdgcn_readfirstlane(at)];
-  if (e0 >= row) return;
-  const int run = rec.prefix / SL + (u - rec.unit0);               // run of the sequence's positions
-  const int s0 = rec.prefix > run * SL ? rec.prefix - run * SL : 0;
-  const int end = rec.prefix + rec.n - run * SL, s1 = end < SL ? end : SL;
-  const int t0 = rec.t0 + run * SL + s0 - rec.prefix;              // token of slot s0
+  rec = __builtin_amdgcn_readfirstlane(rec);
+  const int prefix = list.prefix[rec], n = list.t0[rec + 1] - list.t0[rec];
+  const int run = prefix / SL + (u - list.unit0[rec]);             // run of the sequence's positions
+  const int s0 = prefix > run * SL ? prefix - run * SL : 0;
+  const int end = prefix + n - run * SL, s1 = end < SL ? end : SL;
+  const int64_t t0 = (int64_t)list.t0[rec] + run * SL - prefix;    // token of slot 0, were it new
   const int slot0 = run * SL & (a.pb - 1);
-  const int64_t blk = a.tables[(int64_t)rec.seq * a.max_blocks + run * SL / a.pb];
+  const int64_t blk = a.tables[(int64_t)(list.seq0 + rec) * a.max_blocks + run * SL / a.pb];
   uint8_t* const base = a.pool + blk * a.block_bytes;
-  const int g = e0 / D, c0 = e0 - g * D;
-  const float ks = a.k_scale[g], vs = a.v_scale[g], kr = 1.f / ks, vr = 1.f / vs;
-  uint8_t* const kdst = base + ((int64_t)g * a.pb + slot0) * D + c0;
-  uint8_t* const vdst = base + (int64_t)row * a.pb + (int64_t)e0 * a.pb + slot0;
-  const ST* const kn = reinterpret_cast<const ST*>(a.k_new) + (int64_t)t0 * row + e0;
-  const ST* const vn = reinterpret_cast<const ST*>(a.v_new) + (int64_t)t0 * row + e0;
-  const auto word = [&](const ST* p, float s, float r) {
-    ST e[C];
-    __builtin_memcpy(e, __builtin_assume_aligned(p, 8), sizeof(e));
-    float f[C];
+  const auto bytes4 = [](const ST* e, float s, float r) {
+    float f[4];
 #pragma unroll
-    for (int i = 0; i < C; ++i) f[i] = quotient(S::to_float(e[i]), s, r);
+    for (int i = 0; i < 4; ++i) f[i] = quotient(S::to_float(e[i]), s, r);
     uint32_t w = 0;
     w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], w, false);
     w = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
     return w;
   };
-  if (s0 == 0 && s1 == SL) {
-#pragma unroll 8
-    for (int s = 0; s < SL; ++s) *reinterpret_cast<uint32_t*>(kdst + s * D) = word(kn + (int64_t)s * row, ks, kr);
+  if (!is_v) {
+    const int e0 = (blockIdx.y >> 1) * 1024 + (threadIdx.x & 127) * 8, h = threadIdx.x >> 7;
+    if (e0 >= row) return;
+    const int g = e0 / D;
+    const float scale = a.k_scale[g], r = 1.f / scale;
+    uint8_t* const dst = base + ((int64_t)g * a.pb + slot0) * D + (e0 - g * D);
+    const ST* const src = reinterpret_cast<const ST*>(a.k_new) + t0 * row + e0;
+    u32x4 x[16];
 #pragma unroll
-    for (int h = 0; h < SL / 16; ++h) {
-      uint32_t by_slot[16], by_chan[C][4];
+    for (int i = 0; i < 16; ++i) {
+      const int s = 16 * h + i;
+      if (s >= s0 && s < s1) x[i] = *reinterpret_cast<const u32x4*>(src + (int64_t)s * row);
+    }
 #pragma unroll
-      for (int s = 0; s < 16; ++s) by_slot[s] = word(vn + (int64_t)(16 * h + s) * row, vs, vr);
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          uint32_t w = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w |= ((by_slot[4 * q + i] >> (8 * c)) & 0xffu) << (8 * i);
-          by_chan[c][q] = w;
-        }
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        *reinterpret_cast<u32x4*>(vdst + (int64_t)c * a.pb + 16 * h) = u32x4{by_chan[c][0], by_chan[c][1], by_chan[c][2], by_chan[c][3]};
+    for (int i = 0; i < 16; ++i) {
+      const int s = 16 * h + i;
+      if (s < s0 || s >= s1) continue;
+      ST e[8];
+      __builtin_memcpy(e, &x[i], 16);
+      *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = make_uint2(bytes4(e, scale, r), bytes4(e + 4, scale, r));
     }
     return;
   }
-  for (int s = s0; s < s1; ++s) {
-    *reinterpret_cast<uint32_t*>(kdst + s * D) = word(kn + (int64_t)(s - s0) * row, ks, kr);
-    const uint32_t w = word(vn + (int64_t)(s - s0) * row, vs, vr);
+  const int e0 = (blockIdx.y >> 1) * 1024 + threadIdx.x * 4;
+  if (e0 >= row) return;
+  const float scale = a.v_scale[e0 / D], r = 1.f / scale;
+  uint8_t* const dst = base + (int64_t)row * a.pb + (int64_t)e0 * a.pb + slot0;
+  const ST* const src = reinterpret_cast<const ST*>(a.v_new) + t0 * row + e0;
+  const auto fetch = [&](int s) { return *reinterpret_cast<const uint2*>(src + (int64_t)s * row); };
+  const auto word = [&](uint2 x) {
+    ST e[4];
+    __builtin_memcpy(e, &x, 8);
+    return bytes4(e, scale, r);
+  };
+  if (s1 - s0 <= 2) {
+    for (int s = s0; s < s1; ++s) {
+      const uint32_t w = word(fetch(s));
 #pragma unroll
-    for (int c = 0; c < C; ++c) vdst[(int64_t)c * a.pb + s] = (uint8_t)(w >> (8 * c));
+      for (int c = 0; c < 4; ++c) dst[(int64_t)c * a.pb + s] = (uint8_t)(w >> (8 * c));
+    }
+    return;
+  }
+  uint2 x[SL];
+#pragma unroll
+  for (int s = 0; s < SL; ++s)
+    if (s >= s0 && s < s1) x[s] = fetch(s);
+#pragma unroll
+  for (int h = 0; h < SL / 16; ++h) {
+    if (s1 <= 16 * h || s0 >= 16 * h + 16) continue;
+    uint32_t by_slot[16];
+#pragma unroll
+    for (int s = 0; s < 16; ++s) by_slot[s] = word(x[16 * h + s]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      u32x4* const at = reinterpret_cast<u32x4*>(dst + (int64_t)c * a.pb + 16 * h);
+      u32x4 w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t b = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b |= ((by_slot[4 * q + i] >> (8 * c)) & 0xffu) << (8 * i);
+        w[q] = b;
+      }
+      if (s0 > 16 * h || s1 < 16 * h + 16) {
+        const u32x4 old = *at;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t mask = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mask |= 16 * h + 4 * q + i >= s0 && 16 * h + 4 * q + i < s1 ? 0xffu << (8 * i) : 0u;
+          w[q] = (w[q] & mask) | (old[q] & ~mask);
+        }
+      }
+      *at = w;
+    }
   }
 }
 
@@ -99,17 +136,17 @@ __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpStepL
 // walks the path.  Places are taken in increasing order and a place is never behind the token that comes to it, so nothing is
 // overwritten before it is read; four moves are read together and then stored, which keeps that.
 template <int ES, int D>
-__global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpStepList list, const int32_t* __restrict__ n_accept,
+__global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpSeqList list, const int32_t* __restrict__ n_accept,
                                                         const int32_t* __restrict__ path) {
   typedef typename std::conditional<ES == 4, uint32_t, typename std::conditional<ES == 2, uint16_t, uint8_t>::type>::type E;
   constexpr int C = 16 / ES;
-  const FlpStepSeq* __restrict__ recs = a.recs ? a.recs : list.seq;
-  const FlpStepSeq rec = recs[blockIdx.x];
+  const int seq = list.seq0 + blockIdx.x, prefix = list.prefix[blockIdx.x];
+  const int t0 = list.t0[blockIdx.x], n = list.t0[blockIdx.x + 1] - t0;
   const int row = a.n_kv * D, e0 = (blockIdx.y * 256 + threadIdx.x) * C;
-  if (e0 >= row) return;
-  const int taken = n_accept[rec.seq], m = taken < rec.n ? taken : rec.n;
-  const int32_t* const p = path + rec.t0;
-  const int32_t* const table = a.tables + (int64_t)rec.seq * a.max_blocks;
+  if (e0 >= row || n == 0) return;
+  const int taken = n_accept[seq], m = taken < n ? taken : n;
+  const int32_t* const p = path + t0;
+  const int32_t* const table = a.tables + (int64_t)seq * a.max_blocks;
   const int g = e0 / D, c0 = e0 - g * D, psh = __builtin_ctz(a.pb);
   const int64_t koff = ((int64_t)g * a.pb * D + c0) * ES, voff = ((int64_t)row * a.pb + (int64_t)e0 * a.pb) * ES;
   constexpr int B = 4;
@@ -121,10 +158,10 @@ __global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpStepLi
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       const int j = j0 + b, src = j < m ? p[j] : -1;
-      on = on && src >= 0 && src < rec.n;
+      on = on && src >= 0 && src < n;
       move[b] = on && src != j;
       if (!move[b]) continue;
-      const int pos = rec.prefix + src, slot = pos & (a.pb - 1);
+      const int pos = prefix + src, slot = pos & (a.pb - 1);
       const uint8_t* const blk = a.pool + (int64_t)table[pos >> psh] * a.block_bytes;
       k[b] = *reinterpret_cast<const u32x4*>(blk + koff + (int64_t)slot * D * ES);
 #pragma unroll
@@ -133,7 +170,7 @@ __global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpStepLi
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       if (!move[b]) continue;
-      const int pos = rec.prefix + j0 + b, slot = pos & (a.pb - 1);
+      const int pos = prefix + j0 + b, slot = pos & (a.pb - 1);
       uint8_t* const blk = a.pool + (int64_t)table[pos >> psh] * a.block_bytes;
       *reinterpret_cast<u32x4*>(blk + koff + (int64_t)slot * D * ES) = k[b];
 #pragma unroll
@@ -144,10 +181,10 @@ __global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpStepLi
 
 }  // namespace
 
-flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int64_t n_units,
+flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, int32_t n_units,
                                  hipStream_t stream) {
   if (n_units <= 0) return FLP_OK;
-  const dim3 grid((unsigned)n_units, (unsigned)((a.n_kv * head_dim + 1023) / 1024));
+  const dim3 grid((unsigned)n_units, 2 * (unsigned)((a.n_kv * head_dim + 1023) / 1024));
   const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, list); };
   if (dtype == FLP_F16)
     head_dim == 64 ? launch(kv_append8_kernel<F16, 64>) : launch(kv_append8_kernel<F16, 128>);
@@ -157,11 +194,11 @@ flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, 
   return FLP_OK;
 }
 
-flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpStepList& list, const int32_t* n_accept,
+flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, const int32_t* n_accept,
                                 const int32_t* path, hipStream_t stream) {
-  if (a.n_recs <= 0) return FLP_OK;
+  if (list.n <= 0) return FLP_OK;
   const int per = 256 * 16 / elem_bytes;
-  const dim3 grid((unsigned)a.n_recs, (unsigned)((a.n_kv * head_dim + per - 1) / per));
+  const dim3 grid((unsigned)list.n, (unsigned)((a.n_kv * head_dim + per - 1) / per));
   const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, list, n_accept, path); };
   if (elem_bytes == 1)
     head_dim == 64 ? launch(kv_accept_kernel<1, 64>) : launch(kv_accept_kernel<1, 128>);

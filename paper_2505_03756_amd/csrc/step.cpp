@@ -115,12 +115,6 @@ FlpStepArgs make_args(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_
   return a;
 }
 
-// Where a launch finds its records: in its own arguments, or behind them in one staging slot of the call
-struct Staged {
-  FlpStageSlot* slot = nullptr;
-  size_t used = 0;
-};
-
 bool inline_records(const std::vector<FlpStepSeq>& recs) { return recs.size() <= (size_t)kStepInline; }
 
 // Staging slots and the workspace are handed from call to call by events, which a replayed graph would not see
@@ -134,27 +128,31 @@ flp_status refuse_capture(hipStream_t stream, const char* who) {
   return FLP_OK;
 }
 
-// The records of one launch, in `list` or at the next place of the slot
-void place(Staged& st, const std::vector<FlpStepSeq>& recs, FlpStepArgs* a, FlpStepList* list) {
-  a->n_recs = (int32_t)recs.size();
-  const size_t bytes = recs.size() * sizeof(FlpStepSeq);
-  if (inline_records(recs)) {
-    memcpy(list->seq, recs.data(), bytes);
-    return;
+// The sequences of one append or accept launch, from sequence `first` of the batch on; returns the units of its append, the runs of
+// kAppend8Slots positions that get new slots
+int64_t seq_list(const flp_attn_batch* b, int32_t first, FlpSeqList* l) {
+  l->seq0 = first;
+  l->n = std::min(kListSeqs, b->n_seqs - first);
+  int64_t units = 0;
+  for (int32_t i = 0; i < l->n; ++i) {
+    const int32_t prefix = b->prefix_len[first + i], n = b->cu_new[first + i + 1] - b->cu_new[first + i];
+    l->t0[i] = b->cu_new[first + i];
+    l->prefix[i] = prefix;
+    l->unit0[i] = (int32_t)units;
+    if (n > 0) units += (prefix + n - 1) / kAppend8Slots - prefix / kAppend8Slots + 1;
   }
-  memcpy((uint8_t*)st.slot->host + st.used, recs.data(), bytes);
-  a->recs = (const FlpStepSeq*)((const uint8_t*)st.slot->dev + st.used);
-  st.used += bytes;
+  l->t0[l->n] = b->cu_new[first + l->n];
+  return units;
 }
 
-// units of the append: the runs of kAppend8Slots positions that get new slots
-int64_t append_plan(std::vector<FlpStepSeq>& recs) {
-  int64_t n = 0;
-  for (FlpStepSeq& r : recs) {
-    r.unit0 = (int32_t)n;
-    n += (r.prefix + r.n - 1) / kAppend8Slots - r.prefix / kAppend8Slots + 1;
+flp_status append8(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, hipStream_t stream) {
+  const FlpStepArgs a = make_args(p, b, sc, true);
+  FlpSeqList list;
+  for (int32_t first = 0; first < b->n_seqs; first += kListSeqs) {
+    const int64_t units = seq_list(b, first, &list);   // below 2^31: so are the new tokens
+    FLP_TRY(flp_launch_kv_append8(p->cfg.dtype, p->cfg.head_dim, a, list, (int32_t)units, stream));
   }
-  return n;
+  return FLP_OK;
 }
 
 // One launch of the attention kernel
@@ -210,59 +208,57 @@ std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, cons
   return launches;
 }
 
-// An append, an attention, or both in this order, of a batch that has passed the checks
-flp_status run(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, const uint64_t* mask, bool append8, bool attend,
-               const std::vector<FlpStepSeq>& recs, hipStream_t stream, const char* who) {
+// The attention of a batch that has passed the checks; with_append8: K and V of the new tokens are stored in 8 bits before it
+flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, const uint64_t* mask, bool with_append8,
+                  const std::vector<FlpStepSeq>& recs, hipStream_t stream, const char* who) {
   std::lock_guard<std::mutex> lk(p->mu);
-  std::vector<FlpStepSeq> add;
-  int64_t add_units = 0;
-  if (append8) {
-    add = recs;
-    add_units = append_plan(add);
-  }
-  std::vector<AttnLaunch> launches;
   size_t part_rows = 0;
-  if (attend) launches = attn_plan(p, b->n_q_heads / p->cfg.n_kv_heads, sc ? 1 : p->elem_bytes, recs, &part_rows);
-  for (const AttnLaunch& l : launches)
+  const std::vector<AttnLaunch> launches = attn_plan(p, b->n_q_heads / p->cfg.n_kv_heads, sc ? 1 : p->elem_bytes, recs, &part_rows);
+  size_t staged = 0;
+  for (const AttnLaunch& l : launches) {
     if (l.units * p->cfg.n_kv_heads > INT32_MAX || (int64_t)l.merge_rows * b->n_q_heads > INT32_MAX) {
       flp_set_error("%s: more rows than one launch takes", who);
       return FLP_ERANGE;
     }
-  size_t staged = inline_records(add) ? 0 : add.size();
-  for (const AttnLaunch& l : launches) staged += inline_records(l.recs) ? 0 : l.recs.size();
-  Staged st;
-  float* partials = nullptr;
+    staged += inline_records(l.recs) ? 0 : l.recs.size();
+  }
+  FlpStageSlot* slot = nullptr;
+  FlpStepArgs a = make_args(p, b, sc, sc != nullptr);
+  a.mask = mask;
   if (staged || part_rows) {
     FLP_TRY(refuse_capture(stream, who));
     if (part_rows) {
       void* w = nullptr;
       FLP_TRY(flp_attn_workspace(p, part_rows * b->n_q_heads * (p->cfg.head_dim + 2) * sizeof(float), stream, &w));
-      partials = (float*)w;
+      a.partials = (float*)w;
     }
-    FLP_TRY(flp_stage_acquire(p, staged * sizeof(FlpStepSeq), &st.slot));
+    FLP_TRY(flp_stage_acquire(p, staged * sizeof(FlpStepSeq), &slot));
+    FlpStepSeq* to = (FlpStepSeq*)slot->host;
+    for (const AttnLaunch& l : launches)
+      if (!inline_records(l.recs)) to = std::copy(l.recs.begin(), l.recs.end(), to);
   }
-  // every launch's records first, then one upload of what is staged
-  FlpStepArgs base = make_args(p, b, sc, sc != nullptr), add_args = base;
-  base.mask = mask;
-  base.partials = partials;
-  FlpStepList lists[3];
-  std::vector<FlpStepArgs> args;
-  if (append8) place(st, add, &add_args, &lists[2]);
-  for (const AttnLaunch& l : launches) {
-    FlpStepArgs a = base;
+  flp_status s = staged ? flp_stage_upload(slot, staged * sizeof(FlpStepSeq), stream) : FLP_OK;
+  if (s == FLP_OK && with_append8) s = append8(p, b, sc, stream);
+  const FlpStepSeq* at = slot ? (const FlpStepSeq*)slot->dev : nullptr;
+  for (size_t i = 0; i < launches.size() && s == FLP_OK; ++i) {
+    const AttnLaunch& l = launches[i];
+    FlpStepList list;
+    a.n_recs = (int32_t)l.recs.size();
     a.merge_rows = l.merge_rows;
     a.row_waves = l.row_waves;
-    place(st, l.recs, &a, &lists[args.size()]);
-    args.push_back(a);
+    a.recs = nullptr;
+    if (inline_records(l.recs)) {
+      std::copy(l.recs.begin(), l.recs.end(), list.seq);
+    } else {
+      a.recs = at;
+      at += l.recs.size();
+    }
+    s = flp_launch_attn_step(p->cfg.dtype, p->cfg.head_dim, a, list, l.row_tiles, l.units, stream);
   }
-  flp_status s = staged ? flp_stage_upload(st.slot, st.used, stream) : FLP_OK;
-  if (s == FLP_OK && append8) s = flp_launch_kv_append8(p->cfg.dtype, p->cfg.head_dim, add_args, lists[2], add_units, stream);
-  for (size_t i = 0; i < launches.size() && s == FLP_OK; ++i)
-    s = flp_launch_attn_step(p->cfg.dtype, p->cfg.head_dim, args[i], lists[i], launches[i].row_tiles, launches[i].units, stream);
-  if (!st.slot) return s;
-  const flp_status released = flp_stage_release(st.slot, stream);
+  if (!slot) return s;
+  const flp_status released = flp_stage_release(slot, stream);
   if (part_rows && released == FLP_OK) {
-    p->attn_slot = st.slot;
+    p->attn_slot = slot;
     p->attn_stream = stream;
   }
   return s != FLP_OK ? s : released;
@@ -294,7 +290,7 @@ extern "C" flp_status flp_kv_append8(flp_pool* p, const flp_attn_batch* b, const
     FLP_TRY(check_batch(p, b, sc, Call{who, true, false, true, 0}, &recs));
     if (recs.empty()) return FLP_OK;
     FLP_TRY(check_device(p, who));
-    return run(p, b, sc, nullptr, true, false, recs, (hipStream_t)hip_stream, who);
+    return append8(p, b, sc, (hipStream_t)hip_stream);
   });
 }
 
@@ -310,7 +306,7 @@ extern "C" flp_status flp_paged_prefix_attention8(flp_pool* p, const flp_attn_ba
     FLP_TRY(check_batch(p, b, sc, Call{who, true, true, append, 0}, &recs));
     if (recs.empty()) return FLP_OK;
     FLP_TRY(check_device(p, who));
-    return run(p, b, sc, nullptr, append, true, recs, (hipStream_t)hip_stream, who);
+    return attend(p, b, sc, nullptr, append, recs, (hipStream_t)hip_stream, who);
   });
 }
 
@@ -331,7 +327,7 @@ extern "C" flp_status flp_paged_tree_attention(flp_pool* p, const flp_attn_batch
       FLP_TRY(refuse_capture((hipStream_t)hip_stream, who));
       FLP_TRY(flp_kv_append(p, b, hip_stream));
     }
-    return run(p, b, sc, tree_mask, append && sc, true, recs, (hipStream_t)hip_stream, who);
+    return attend(p, b, sc, tree_mask, append && sc, recs, (hipStream_t)hip_stream, who);
   });
 }
 
@@ -352,13 +348,10 @@ extern "C" flp_status flp_kv_accept(flp_pool* p, const flp_attn_batch* b, const 
     }
     FLP_TRY(check_device(p, who));
     hipStream_t stream = (hipStream_t)hip_stream;
-    const FlpStepArgs a0 = make_args(p, b, nullptr, kv8 == 1);
-    // sequences are independent: as many launches as the arguments' records take
-    for (size_t i = 0; i < recs.size(); i += kStepInline) {
-      FlpStepArgs a = a0;
-      FlpStepList list;
-      a.n_recs = (int32_t)std::min<size_t>(kStepInline, recs.size() - i);
-      memcpy(list.seq, recs.data() + i, a.n_recs * sizeof(FlpStepSeq));
+    const FlpStepArgs a = make_args(p, b, nullptr, kv8 == 1);
+    FlpSeqList list;
+    for (int32_t first = 0; first < b->n_seqs; first += kListSeqs) {
+      seq_list(b, first, &list);
       FLP_TRY(flp_launch_kv_accept(kv8 ? 1 : p->elem_bytes, p->cfg.head_dim, a, list, n_accept, path, stream));
     }
     return FLP_OK;
