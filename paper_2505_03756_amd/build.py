@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libflpool.so")
 SOURCES = ["pool.cpp", "dispatch.cpp", "step.cpp", "cache_manager.cpp", "sched.cpp", "swap.hip", "attention.hip", "attention_mfma.hip",
-           "attention_decode.hip", "attention_step.hip", "kv8.hip", "lora.hip", "lora_mfma.hip", "lora_small.hip", "gemm.hip", "layer.hip",
+           "attention_decode.hip", "attention_step.hip", "attention_step_tiles.hip", "kv8.hip", "lora.hip", "lora_mfma.hip", "lora_small.hip", "gemm.hip", "layer.hip",
            "static_scratch.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,

@@ -39,91 +39,29 @@
 #include <hip/hip_runtime.h>
 
 #include "attention_decode_wave.h"
+#include "attention_tile.h"
 #include "flp_internal.h"
 #include "flp_types.h"
 
 namespace {
 
-constexpr int D = 128;
-constexpr int BT = 16;
-constexpr int BN = 64;                 // keys per tile
-constexpr int kTile = BN * D * 2;      // bytes of one K (or V) tile: 16 KiB
-constexpr int kStage = 2 * kTile;      // K tile followed by V tile
+using namespace flp_tile;
+
 constexpr int kStages = 3;             // tiles in the LDS ring: one being multiplied, kStages - 1 in flight
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
-
-struct MF16 {
-  typedef h16x8 vec;
-  typedef flp_decode::DF16 Single;
-  static __device__ __forceinline__ f32x4 mfma(vec a, vec b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-  }
-  // 8 weights -> 16 bit; adds their sum as seen after rounding
-  static __device__ __forceinline__ vec pack(const float* p, float& sum) {
-    vec v;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (_Float16)p[j];
-    const h16x2 one = {(_Float16)1.f, (_Float16)1.f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_fdot2(h16x2{v[2 * j], v[2 * j + 1]}, one, sum, false);
-    return v;
-  }
-  static __device__ __forceinline__ uint16_t out(float f) { return F16::from_float(f); }
-};
-struct MBF16 {
-  typedef b16x8 vec;
-  typedef flp_decode::DBF16 Single;
-  static __device__ __forceinline__ f32x4 mfma(vec a, vec b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ vec pack(const float* p, float& sum) {
-    vec v;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (__bf16)p[j];
-    const b16x2 one = {(__bf16)1.f, (__bf16)1.f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_fdot2_f32_bf16(b16x2{v[2 * j], v[2 * j + 1]}, one, sum, false);
-    return v;
-  }
-  static __device__ __forceinline__ uint16_t out(float f) { return BF16::from_float(f); }
-};
-
-template <typename V>
-__device__ __forceinline__ V as_vec(u32x4 r) {
-  V v;
-  __builtin_memcpy(&v, &r, 16);
-  return v;
-}
-
-// XOR term of the K row swizzle: the key's row of its A operand
-__device__ __forceinline__ int k_swz(int key32) { return ((key32 >> 3) << 2) | (key32 & 3); }
-__device__ __forceinline__ int v_swz(int d) { return ((d >> 2) & 1) ^ ((d >> 3) & 1); }
 
 // s_waitcnt immediates (gfx9 encoding: vmcnt[3:0] + [15:14], expcnt[6:4], lgkmcnt[11:8]), other counters untouched
 constexpr int kWaitTile = (4 * (kStages - 2)) | (7 << 4) | (15 << 8);   // all but the newest kStages - 2 tiles (4 loads each) have landed
 constexpr int kScheduleAlu = 6;        // __builtin_amdgcn_sched_barrier: vector and scalar arithmetic may cross
 constexpr int kWaitVm0 = 0 | (7 << 4) | (15 << 8);
 
-// One direct global-to-LDS load: every lane fetches 16 bytes from base + voff and the wave's 64
-// pieces land at LDS byte address lds .. lds + 1023 in lane order (base and lds wave-uniform).
-// Written as inline assembly on purpose: the compiler does not see these loads, so it neither
-// counts them in its own memory-counter waits nor makes every later LDS read wait for all of
-// them; the kernel orders them against the LDS reads itself (s_waitcnt vmcnt + barrier).
-// M0 is named as clobbered so that no pass keeps a value of its own alive in it across the statement; the
-// compiler notes that it reserves the register, which is the point.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_to_lds16(const void* base, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds)
-               : "memory", "m0");
-}
-#pragma clang diagnostic pop
-typedef __attribute__((address_space(3))) uint8_t lds_u8;
+template <typename M>
+struct Single {
+  typedef flp_decode::DF16 type;
+};
+template <>
+struct Single<MBF16> {
+  typedef flp_decode::DBF16 type;
+};
 
 template <typename M>
 __global__ __launch_bounds__(512, 2) void attn_mfma_kernel(FlpAttnArgs a, const FlpMfmaItem* __restrict__ items,
@@ -138,7 +76,7 @@ __global__ __launch_bounds__(512, 2) void attn_mfma_kernel(FlpAttnArgs a, const 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (it.n_rows < 0) {                                 // single tokens: (unit, kv head) pairs r0 .. r0 + 7 of `seq`
     const int pair = it.r0 + wave;
-    if (pair < it.seq) flp_decode::decode_unit<typename M::Single>(a, units[pair / a.n_kv], pair % a.n_kv);
+    if (pair < it.seq) flp_decode::decode_unit<typename Single<M>::type>(a, units[pair / a.n_kv], pair % a.n_kv);
     return;                                            // waves share nothing
   }
   const int G = a.n_h / a.n_kv, g = it.g;

@@ -29,6 +29,7 @@
 
 #include <type_traits>
 
+#include "attention_step_record.h"
 #include "flp_internal.h"
 #include "flp_types.h"
 
@@ -103,18 +104,6 @@ __device__ __forceinline__ float got(float v, int) { return v; }
 __device__ __forceinline__ float got(h16x8 v, int e) { return (float)v[e]; }
 __device__ __forceinline__ float got(b16x8 v, int e) { return (float)v[e]; }
 
-// The record that workgroup unit `u` belongs to: the last one whose first unit is not behind u
-__device__ __forceinline__ int find(const FlpStepSeq* __restrict__ recs, int n, int u, int FlpStepSeq::*first) {
-  int at = -1;
-  for (int base = 0; base < n; base += 64) {
-    const int i = base + (threadIdx.x & 63);
-    const unsigned long long le = __builtin_amdgcn_ballot_w64(i < n && recs[i].*first <= u);
-    at += __builtin_popcountll(le);
-    if (le != ~0ull) break;
-  }
-  return __builtin_amdgcn_readfirstlane(at);
-}
-
 template <typename S, int D, int J, bool KV8>
 __global__ __launch_bounds__(256, J == 1 ? 2 : 1) void attn_step_kernel(FlpStepArgs a, FlpStepList list) {
   typedef Kind<S, KV8> C;
@@ -129,8 +118,7 @@ __global__ __launch_bounds__(256, J == 1 ? 2 : 1) void attn_step_kernel(FlpStepA
   const int lane = threadIdx.x & 63, lr = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int u = blockIdx.x / a.n_kv, g = blockIdx.x - u * a.n_kv;
-  const FlpStepSeq* __restrict__ recs = a.recs ? a.recs : list.seq;
-  const FlpStepSeq rec = recs[find(recs, a.n_recs, u, &FlpStepSeq::unit0)];
+  const FlpStepSeq rec = flp_step_record(a, list, u, &FlpStepSeq::unit0);
   const int G = a.n_h / a.n_kv, R = rec.n * G, P = rec.prefix, L = P + rec.n;
   const int rw = a.row_waves, kw = 4 / rw;             // waves side by side on row tiles, and on slices of the context
   const int groups = (R + 16 * J * rw - 1) / (16 * J * rw);      // workgroups that the rows take
@@ -505,8 +493,7 @@ __global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, Flp
   const int64_t wid = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = (int)(wid / a.n_h), h = (int)(wid - (int64_t)row * a.n_h);
   if (row >= a.merge_rows) return;
-  const FlpStepSeq* __restrict__ recs = a.recs ? a.recs : list.seq;
-  const FlpStepSeq rec = recs[find(recs, a.n_recs, row, &FlpStepSeq::merge0)];
+  const FlpStepSeq rec = flp_step_record(a, list, row, &FlpStepSeq::merge0);
   const int tok = row - rec.merge0, ns = rec.pieces;
   const int64_t stride = (int64_t)a.n_h * (D + 2);
   const float* __restrict__ pp = a.partials + ((int64_t)rec.part0 + (int64_t)tok * ns) * stride + (int64_t)h * (D + 2);
@@ -576,7 +563,12 @@ flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, c
   else
     d64 ? launch_kind<BF16, 64>(a, list, row_tiles, grid, stream) : launch_kind<BF16, 128>(a, list, row_tiles, grid, stream);
   FLP_TRY_HIP(hipGetLastError());
+  return FLP_OK;
+}
+
+flp_status flp_launch_attn_step_merge(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, hipStream_t stream) {
   if (a.merge_rows <= 0) return FLP_OK;
+  const bool d64 = head_dim == 64;
   const dim3 mgrid((unsigned)(((int64_t)a.merge_rows * a.n_h + 3) / 4));
   const auto merge = [&](auto kernel) { hipLaunchKernelGGL(kernel, mgrid, dim3(256), 0, stream, a, list); };
   if (dtype == FLP_F32)

@@ -240,6 +240,10 @@ struct FlpStepArgs {
 // row_tiles (1, 2 or 4): tiles of 16 query rows per wave
 flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles,
                                 int64_t n_units, hipStream_t stream);
+// many query rows per kv head: 16-bit types, head_dim 128, contexts of up to kMfmaMaxBlocks blocks; units of kMfmaRowsPerItem rows
+flp_status flp_launch_attn_step_tiles(int dtype, const FlpStepArgs& a, const FlpStepList& list, int64_t n_units, hipStream_t stream);
+// the pieces of a launch of either kind that has merge rows
+flp_status flp_launch_attn_step_merge(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, hipStream_t stream);
 constexpr int kAppend8Slots = 32;      // a unit of the 8-bit append: the slots of one such run of positions
 flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, int32_t n_units,
                                  hipStream_t stream);

@@ -155,44 +155,50 @@ flp_status append8(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_sca
   return FLP_OK;
 }
 
-// One launch of the attention kernel
+// One launch of an attention kernel
 struct AttnLaunch {
   std::vector<FlpStepSeq> recs;
+  bool tiles;                  // attention_step_tiles.hip
   int32_t row_tiles, row_waves, merge_rows;
   int64_t units;
 };
 
-// Sequences with up to 64 query rows per kv head go in one launch, those with more in another: the first has a wave take all rows and the
-// workgroup's four waves a slice of the context each, the second has the waves share K and V between row tiles.
-// Contexts are cut into pieces of equal length, at least kMinPiece tiles for every wave, so that a launch has about kUnits workgroups.
-constexpr int64_t kUnits = 1024;
-constexpr int kMinPiece = 4, kMaxPieces = 64;
+// Sequences with many query rows per kv head go to the tiled kernel, the others to the one that reads K and V straight to registers.
+// Contexts are cut into pieces of equal length so that a launch has about kUnits workgroups.
+constexpr int64_t kUnits = 1024, kTileUnits = 512;
+constexpr int kMinPiece = 4, kMinTilePiece = 8, kMaxPieces = 64;
 constexpr int kFewRows = 64;
 
 std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, const std::vector<FlpStepSeq>& all, size_t* part_rows) {
   std::vector<AttnLaunch> launches;
-  const int tile = 64 / elem_bytes, n_kv = p->cfg.n_kv_heads;
+  const int n_kv = p->cfg.n_kv_heads, pb = p->cfg.block_tokens * (p->elem_bytes / elem_bytes);
+  const bool tiles_ok = p->elem_bytes == 2 && p->cfg.head_dim == 128;
+  const auto tiled = [&](const FlpStepSeq& r) {
+    return tiles_ok && (int64_t)r.n * G > kFewRows && ((int64_t)r.prefix + r.n + pb - 1) / pb <= kMfmaMaxBlocks;
+  };
   int64_t parts = 0;
-  for (int many = 1; many >= 0; --many) {
+  for (int tiles = 1; tiles >= 0; --tiles) {
     AttnLaunch l{};
     int64_t rows = 0;
     for (const FlpStepSeq& r : all)
-      if (((int64_t)r.n * G > kFewRows) == (many == 1)) {
+      if (tiled(r) == (tiles == 1)) {
         l.recs.push_back(r);
         rows = std::max<int64_t>(rows, (int64_t)r.n * G);
       }
     if (l.recs.empty()) continue;
+    l.tiles = tiles == 1;
     l.row_tiles = rows <= 16 ? 1 : rows <= 32 || elem_bytes == 4 ? 2 : 4;      // fp32: four tiles do not fit the registers
     l.row_waves = rows <= 16 * l.row_tiles ? 1 : rows <= 32 * l.row_tiles ? 2 : 4;
-    const int per_group = 16 * l.row_tiles * l.row_waves;
-    const auto tiles = [&](const FlpStepSeq& r) { return ((int64_t)r.prefix + r.n + tile - 1) / tile; };
+    const int tile = l.tiles ? 64 : 64 / elem_bytes, per_group = l.tiles ? kMfmaRowsPerItem : 16 * l.row_tiles * l.row_waves;
+    const auto tiles_of = [&](const FlpStepSeq& r) { return ((int64_t)r.prefix + r.n + tile - 1) / tile; };
     const auto groups = [&](const FlpStepSeq& r) { return ((int64_t)r.n * G + per_group - 1) / per_group; };
-    std::stable_sort(l.recs.begin(), l.recs.end(), [&](const FlpStepSeq& x, const FlpStepSeq& y) { return tiles(x) > tiles(y); });
+    std::stable_sort(l.recs.begin(), l.recs.end(), [&](const FlpStepSeq& x, const FlpStepSeq& y) { return tiles_of(x) > tiles_of(y); });
     int64_t total = 0;
-    for (const FlpStepSeq& r : l.recs) total += groups(r) * tiles(r) * n_kv;
-    const int64_t piece = std::max<int64_t>(kMinPiece * (4 / l.row_waves), (total + kUnits - 1) / kUnits);
+    for (const FlpStepSeq& r : l.recs) total += groups(r) * tiles_of(r) * n_kv;
+    const int64_t piece = l.tiles ? std::max<int64_t>(kMinTilePiece, (total + kTileUnits - 1) / kTileUnits)
+                                  : std::max<int64_t>(kMinPiece * (4 / l.row_waves), (total + kUnits - 1) / kUnits);
     for (FlpStepSeq& r : l.recs) {
-      r.pieces = (int32_t)std::min<int64_t>(kMaxPieces, (tiles(r) + piece - 1) / piece);
+      r.pieces = (int32_t)std::min<int64_t>(kMaxPieces, (tiles_of(r) + piece - 1) / piece);
       r.unit0 = (int32_t)l.units;
       l.units += groups(r) * r.pieces;
       r.part0 = (int32_t)parts;
@@ -253,7 +259,9 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
       a.recs = at;
       at += l.recs.size();
     }
-    s = flp_launch_attn_step(p->cfg.dtype, p->cfg.head_dim, a, list, l.row_tiles, l.units, stream);
+    s = l.tiles ? flp_launch_attn_step_tiles(p->cfg.dtype, a, list, l.units, stream)
+                : flp_launch_attn_step(p->cfg.dtype, p->cfg.head_dim, a, list, l.row_tiles, l.units, stream);
+    if (s == FLP_OK) s = flp_launch_attn_step_merge(p->cfg.dtype, p->cfg.head_dim, a, list, stream);
   }
   if (!slot) return s;
   const flp_status released = flp_stage_release(slot, stream);

@@ -4,7 +4,9 @@ float64 oracle.
 Tolerances.  A result is rounded once, by half a step: HALF * |value|.  Before that, attention's scores are sums of d products in fp32
 (off by at most d 2^-24 times the sum of their sizes, `worst`), which moves a weight by as much relative to itself, exp2 by a few
 2^-23, the sums of weights by length * 2^-24 and the pieces that a 16-bit weight is held in by 2^-16 (bf16) or less; a weighted mean
-of values of size vmax moves by at most twice the weights' relative change times vmax."""
+of values of size vmax moves by at most twice the weights' relative change times vmax.  Sequences of more than 64 query rows per kv head
+(16-bit types, head_dim 128) have their weights rounded once to the type of V, fp16 over an 8-bit cache, and summed as rounded: with
+weights w (1 + e), |e| <= HALF, the mean moves by at most 2 HALF vmax."""
 import numpy as np
 import pytest
 import torch
@@ -100,8 +102,10 @@ class Setup:
                 continue
             k, v = self.values(image, i)
             ref, worst, vmax = so.attention(q[lo:hi], k, v, sees(i), scale)
+            once = self.dtype != "f32" and self.d == 128 and n * self.nq // self.nkv > 64
+            pieces = 0 if self.dtype == "f32" else 2 * HALF["f16" if self.kv8 else self.dtype] if once else 2.0 ** -16
             tol = HALF[self.dtype] * np.abs(ref) + TINY[self.dtype] + vmax * (
-                2 * (self.d * 2.0 ** -24 * worst + 2.0 ** -20 + (p + n) * 2.0 ** -24) + (0 if self.dtype == "f32" else 2.0 ** -16))[..., None]
+                2 * (self.d * 2.0 ** -24 * worst + 2.0 ** -20 + (p + n) * 2.0 ** -24) + pieces)[..., None]
             mine = got[lo:hi]
             fin = np.isfinite(ref)
             assert np.array_equal(np.isnan(mine), np.isnan(ref)) and np.array_equal(mine[~fin & ~np.isnan(ref)], ref[~fin & ~np.isnan(ref)]), i
