@@ -18,7 +18,7 @@
 //            words of V are looked over first and what is not finite goes another way (below).
 //   8 bit    e4m3 is exact in fp16 and in bf16: K is widened to the type of q, V and the weights to fp16, two pieces as well.
 //
-// A workgroup is four waves: row tiles x slices of the context, so that waves of different row tiles read the same K and V at about
+// A workgroup is four waves (eight in small launches): row tiles x slices of the context, so that waves of different row tiles read the same K and V at about
 // the same time, and slices are merged in LDS.  Long contexts of small launches are cut into pieces over workgroups as well, which
 // a second launch merges in piece order.  Bound by the traffic of K and V up to 32 rows or so per kv head.
 //
@@ -104,23 +104,23 @@ __device__ __forceinline__ float got(float v, int) { return v; }
 __device__ __forceinline__ float got(h16x8 v, int e) { return (float)v[e]; }
 __device__ __forceinline__ float got(b16x8 v, int e) { return (float)v[e]; }
 
-template <typename S, int D, int J, bool KV8>
-__global__ __launch_bounds__(256, J == 1 ? 2 : 1) void attn_step_kernel(FlpStepArgs a, FlpStepList list) {
+template <typename S, int D, int J, bool KV8, int W>
+__global__ __launch_bounds__(64 * W, J == 1 ? 2 : 1) void attn_step_kernel(FlpStepArgs a, FlpStepList list) {
   typedef Kind<S, KV8> C;
   typedef typename C::kvec kvec;
   typedef typename C::vvec vvec;
   typedef typename S::storage ST;
   constexpr int RUN = 16 / C::ES, TP = 4 * RUN, NT = RUN / 4, KC = D * C::ES / 64, CT = D / 16, STEPS = C::STEPS;
   constexpr int VE = RUN / STEPS;                      // positions of a lane's run that one step of the second product takes
-  __shared__ f32x4 merge_o[4][CT][J][64];
-  __shared__ float2 merge_ml[4][J][16];
+  __shared__ f32x4 merge_o[W][CT][J][64];
+  __shared__ float2 merge_ml[W][J][16];
 
   const int lane = threadIdx.x & 63, lr = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int u = blockIdx.x / a.n_kv, g = blockIdx.x - u * a.n_kv;
   const FlpStepSeq rec = flp_step_record(a, list, u, &FlpStepSeq::unit0);
   const int G = a.n_h / a.n_kv, R = rec.n * G, P = rec.prefix, L = P + rec.n;
-  const int rw = a.row_waves, kw = 4 / rw;             // waves side by side on row tiles, and on slices of the context
+  const int rw = a.row_waves, kw = W / rw;             // waves side by side on row tiles, and on slices of the context
   const int groups = (R + 16 * J * rw - 1) / (16 * J * rw);      // workgroups that the rows take
   const int local = u - rec.unit0, piece = local / groups, rgroup = local - piece * groups;
   const int row0 = (rgroup * rw + wave % rw) * 16 * J, slice = wave / rw;
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(256, J == 1 ? 2 : 1) void attn_step_kernel(FlpStepA
 
   // ---- slices of the context, then the result or the piece's share of it.  Lane (row lr, quarter lh): channels 16 ct + 4 lh ..
   const float vs = KV8 ? a.v_scale[g] : 1.f;
-  float M[J], Lsum[J], factor[J][4];
+  float M[J], Lsum[J], factor[J][W];
   if (kw > 1) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
@@ -427,18 +427,18 @@ __global__ __launch_bounds__(256, J == 1 ? 2 : 1) void attn_step_kernel(FlpStepA
     Lsum[j] = l[j];
     if (kw > 1) {
       const int first = wave % rw;
-      float mm[4], ll[4];
+      float mm[W], ll[W];
       M[j] = -INFINITY;
       Lsum[j] = 0.f;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const float2 v = merge_ml[(first + x * rw) & 3][j][lr];
+      for (int x = 0; x < W; ++x) {
+        const float2 v = merge_ml[(first + x * rw) & (W - 1)][j][lr];
         mm[x] = x < kw ? v.x : -INFINITY;
         ll[x] = v.y;
         M[j] = fmaxf(M[j], mm[x]);
       }
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
+      for (int x = 0; x < W; ++x) {
         factor[j][x] = mm[x] == -INFINITY ? 0.f : mm[x] == M[j] ? 1.f : __builtin_amdgcn_exp2f((mm[x] - M[j]) * c);
         if (x < kw) Lsum[j] += factor[j][x] == 0.f ? (ll[x] != ll[x] ? ll[x] : 0.f) : ll[x] * factor[j][x];
       }
@@ -460,9 +460,9 @@ __global__ __launch_bounds__(256, J == 1 ? 2 : 1) void attn_step_kernel(FlpStepA
         o = f32x4{0.f, 0.f, 0.f, 0.f};
         const int first = wave % rw;
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < W; ++x)
           if (x < kw && factor[j][x] != 0.f) {
-            const f32x4 v = merge_o[(first + x * rw) & 3][ct][j][lane];
+            const f32x4 v = merge_o[(first + x * rw) & (W - 1)][ct][j][lane];
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], factor[j][x], o[i]);
           }
@@ -534,34 +534,37 @@ __global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, Flp
 }
 
 template <typename S, int D, bool KV8>
-void launch_rows(const FlpStepArgs& a, const FlpStepList& list, int row_tiles, unsigned grid, hipStream_t stream) {
+void launch_rows(const FlpStepArgs& a, const FlpStepList& list, int row_tiles, int waves, unsigned grid, hipStream_t stream) {
+  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), 0, stream, a, list); };
   if (row_tiles == 1)
-    hipLaunchKernelGGL((attn_step_kernel<S, D, 1, KV8>), dim3(grid), dim3(256), 0, stream, a, list);
+    waves == 8 ? launch(attn_step_kernel<S, D, 1, KV8, 8>) : launch(attn_step_kernel<S, D, 1, KV8, 4>);
   else if (row_tiles == 2 || std::is_same<S, F32>::value)
-    hipLaunchKernelGGL((attn_step_kernel<S, D, 2, KV8>), dim3(grid), dim3(256), 0, stream, a, list);
+    launch(attn_step_kernel<S, D, 2, KV8, 4>);
   else if constexpr (!std::is_same<S, F32>::value)
-    hipLaunchKernelGGL((attn_step_kernel<S, D, 4, KV8>), dim3(grid), dim3(256), 0, stream, a, list);
+    launch(attn_step_kernel<S, D, 4, KV8, 4>);
 }
 template <typename S, int D>
-void launch_kind(const FlpStepArgs& a, const FlpStepList& list, int row_tiles, unsigned grid, hipStream_t stream) {
+void launch_kind(const FlpStepArgs& a, const FlpStepList& list, int row_tiles, int waves, unsigned grid, hipStream_t stream) {
   if constexpr (!std::is_same<S, F32>::value)
-    if (a.k_scale) return launch_rows<S, D, true>(a, list, row_tiles, grid, stream);
-  launch_rows<S, D, false>(a, list, row_tiles, grid, stream);
+    if (a.k_scale) return launch_rows<S, D, true>(a, list, row_tiles, waves, grid, stream);
+  launch_rows<S, D, false>(a, list, row_tiles, waves, grid, stream);
 }
 
 }  // namespace
 
-flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles,
+flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles, int32_t waves,
                                 int64_t n_units, hipStream_t stream) {
   if (n_units <= 0) return FLP_OK;
   const unsigned grid = (unsigned)(n_units * a.n_kv);
-  const bool d64 = head_dim == 64;
+  const auto launch = [&](auto kind64, auto kind128) {
+    head_dim == 64 ? kind64(a, list, row_tiles, waves, grid, stream) : kind128(a, list, row_tiles, waves, grid, stream);
+  };
   if (dtype == FLP_F32)
-    d64 ? launch_kind<F32, 64>(a, list, row_tiles, grid, stream) : launch_kind<F32, 128>(a, list, row_tiles, grid, stream);
+    launch(launch_kind<F32, 64>, launch_kind<F32, 128>);
   else if (dtype == FLP_F16)
-    d64 ? launch_kind<F16, 64>(a, list, row_tiles, grid, stream) : launch_kind<F16, 128>(a, list, row_tiles, grid, stream);
+    launch(launch_kind<F16, 64>, launch_kind<F16, 128>);
   else
-    d64 ? launch_kind<BF16, 64>(a, list, row_tiles, grid, stream) : launch_kind<BF16, 128>(a, list, row_tiles, grid, stream);
+    launch(launch_kind<BF16, 64>, launch_kind<BF16, 128>);
   FLP_TRY_HIP(hipGetLastError());
   return FLP_OK;
 }

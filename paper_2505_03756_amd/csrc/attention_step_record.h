@@ -4,25 +4,27 @@
 
 #include "flp_internal.h"
 
-// The last record whose `first` (unit0, or merge0) is not behind `at`, in scalar registers; `at` is the same for the whole wave
+// The last record whose `first` (unit0, or merge0) is not behind `at`, in scalar registers; `at` is the same for the whole wave.  Records in the
+// launch's arguments are read there, a single one together with the other arguments.
 __device__ __forceinline__ FlpStepSeq flp_step_record(const FlpStepArgs& a, const FlpStepList& list, int at, int32_t FlpStepSeq::*first) {
-  const FlpStepSeq* __restrict__ recs = a.recs ? a.recs : list.seq;
-  int found = 0;
-  if (a.n_recs > 1) {
-    found = -1;
+  if (a.n_recs == 1) return list.seq[0];
+  const auto search = [&](auto recs) {
+    int found = -1;
     for (int base = 0; base < a.n_recs; base += 64) {
       const int i = base + (threadIdx.x & 63);
-      const unsigned long long le = __builtin_amdgcn_ballot_w64(i < a.n_recs && recs[i].*first <= at);
+      const unsigned long long le = __builtin_amdgcn_ballot_w64(i < a.n_recs && recs(i).*first <= at);
       found += __builtin_popcountll(le);
       if (le != ~0ull) break;
     }
-  }
-  const FlpStepSeq r = recs[__builtin_amdgcn_readfirstlane(found)];
-  int32_t w[sizeof(FlpStepSeq) / 4];
-  __builtin_memcpy(w, &r, sizeof(r));
+    const FlpStepSeq r = recs(__builtin_amdgcn_readfirstlane(found));
+    int32_t w[sizeof(FlpStepSeq) / 4];
+    __builtin_memcpy(w, &r, sizeof(r));
 #pragma unroll
-  for (int i = 0; i < (int)(sizeof(FlpStepSeq) / 4); ++i) w[i] = __builtin_amdgcn_readfirstlane(w[i]);
-  FlpStepSeq out;
-  __builtin_memcpy(&out, w, sizeof(out));
-  return out;
+    for (int i = 0; i < (int)(sizeof(FlpStepSeq) / 4); ++i) w[i] = __builtin_amdgcn_readfirstlane(w[i]);
+    FlpStepSeq out;
+    __builtin_memcpy(&out, w, sizeof(out));
+    return out;
+  };
+  if (a.recs) return search([&](int i) -> const FlpStepSeq& { return a.recs[i]; });
+  return search([&](int i) -> const FlpStepSeq& { return list.seq[i]; });
 }

@@ -225,7 +225,7 @@ struct FlpStepArgs {
   int32_t n_h, n_kv;
   int32_t pb;                  // positions per block of this cache: 16, 32 or 64
   int32_t n_recs, merge_rows;
-  int32_t row_waves;           // attention: waves of a workgroup side by side on row tiles (1, 2 or 4), the others on slices of the context
+  int32_t row_waves;           // attention: waves of a workgroup side by side on row tiles (1, 2 or 4); the others take slices of the context
   float scale_log2e;
   const FlpStepSeq* recs;      // null: in the launch's arguments
   const void* q;
@@ -237,8 +237,8 @@ struct FlpStepArgs {
   const float* v_scale;
   float* partials;             // [piece rows][n_h][head_dim + 2] as in FlpAttnArgs
 };
-// row_tiles (1, 2 or 4): tiles of 16 query rows per wave
-flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles,
+// row_tiles (1, 2 or 4): tiles of 16 query rows per wave; waves of a workgroup: 4, with one row tile also 8
+flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles, int32_t waves,
                                 int64_t n_units, hipStream_t stream);
 // many query rows per kv head: 16-bit types, head_dim 128, contexts of up to kMfmaMaxBlocks blocks; units of kMfmaRowsPerItem rows
 flp_status flp_launch_attn_step_tiles(int dtype, const FlpStepArgs& a, const FlpStepList& list, int64_t n_units, hipStream_t stream);

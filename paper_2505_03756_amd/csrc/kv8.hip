@@ -132,50 +132,73 @@ __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqLi
   }
 }
 
-// One workgroup per (sequence, 256 threads' share of a token's row); a thread owns 16 bytes of K and the channels of these in V and
-// walks the path.  Places are taken in increasing order and a place is never behind the token that comes to it, so nothing is
-// overwritten before it is read; four moves are read together and then stored, which keeps that.
+// One workgroup per (sequence, kv head).  Bound by latency: the path, its length and the blocks that the new tokens lie in are requested
+// together, then 32 places of the path at a time are read, K 16 bytes and V an element per access with neighbouring threads on
+// neighbouring places of a channel, and stored behind a barrier.  A place is never behind the token that comes to it, so what is
+// stored for these places is not read for later ones.
 template <int ES, int D>
 __global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpSeqList list, const int32_t* __restrict__ n_accept,
                                                         const int32_t* __restrict__ path) {
   typedef typename std::conditional<ES == 4, uint32_t, typename std::conditional<ES == 2, uint16_t, uint8_t>::type>::type E;
-  constexpr int C = 16 / ES;
-  const int seq = list.seq0 + blockIdx.x, prefix = list.prefix[blockIdx.x];
-  const int t0 = list.t0[blockIdx.x], n = list.t0[blockIdx.x + 1] - t0;
-  const int row = a.n_kv * D, e0 = (blockIdx.y * 256 + threadIdx.x) * C;
-  if (e0 >= row || n == 0) return;
-  const int taken = n_accept[seq], m = taken < n ? taken : n;
+  constexpr int B = 32, KV = D * ES / 16;              // places at a time; 16-byte pieces of a K row
+  constexpr int NK = B * KV / 256 ? B * KV / 256 : 1, NV = B * D / 256;
+  const int g = blockIdx.x % a.n_kv, i = blockIdx.x / a.n_kv, seq = list.seq0 + i;
+  const int prefix = list.prefix[i], t0 = list.t0[i], n = list.t0[i + 1] - t0;
+  if (n == 0) return;
   const int32_t* const p = path + t0;
   const int32_t* const table = a.tables + (int64_t)seq * a.max_blocks;
-  const int g = e0 / D, c0 = e0 - g * D, psh = __builtin_ctz(a.pb);
-  const int64_t koff = ((int64_t)g * a.pb * D + c0) * ES, voff = ((int64_t)row * a.pb + (int64_t)e0 * a.pb) * ES;
-  constexpr int B = 4;
-  bool on = true;
-  for (int j0 = 0; j0 < m && on; j0 += B) {
-    u32x4 k[B];
-    E v[B][C];
-    bool move[B];
+  const int psh = __builtin_ctz(a.pb), tid = threadIdx.x, lane = tid & 63;
+  const int first = prefix >> psh, blocks = ((prefix + n - 1) >> psh) - first + 1;
+  int src = lane < n ? p[lane] : -1;                   // lane j: the token of place j
+  const int id = lane < blocks ? table[first + lane] : 0;
+  const int taken = n_accept[seq], m = taken < n ? taken : n;
+  const int64_t k0 = (int64_t)g * a.pb * D * ES, v0 = (int64_t)(a.n_kv + g) * a.pb * D * ES;
+  const auto block = [&](int pos) {
+    const int b = (pos >> psh) - first;
+    const int held = __shfl(id, b & 63);
+    return a.pool + (int64_t)(b < 64 ? held : table[first + b]) * a.block_bytes;
+  };
+  for (int j0 = 0; j0 < m; j0 += B) {
+    // the path's next places: lane j holds that of place j0 + j; an entry that is none ends it
+    if (j0) src = lane < B && j0 + lane < m ? p[j0 + lane] : -1;
+    const unsigned long long bad = __builtin_amdgcn_ballot_w64(lane >= B || j0 + lane >= m || src < 0 || src >= n);
+    const int cnt = __builtin_ctzll(bad);              // at most B
+    if (cnt == 0) return;                              // the same for all waves
+    const int wsh = cnt <= 4 ? 2 : cnt <= 8 ? 3 : cnt <= 16 ? 4 : 5;     // 4, 8, 16 or 32 threads side by side on places
+    u32x4 k[NK];
+    E v[NV];
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      const int j = j0 + b, src = j < m ? p[j] : -1;
-      on = on && src >= 0 && src < n;
-      move[b] = on && src != j;
-      if (!move[b]) continue;
-      const int pos = prefix + src, slot = pos & (a.pb - 1);
-      const uint8_t* const blk = a.pool + (int64_t)table[pos >> psh] * a.block_bytes;
-      k[b] = *reinterpret_cast<const u32x4*>(blk + koff + (int64_t)slot * D * ES);
-#pragma unroll
-      for (int c = 0; c < C; ++c) v[b][c] = *reinterpret_cast<const E*>(blk + voff + ((int64_t)c * a.pb + slot) * ES);
+    for (int x = 0; x < NK; ++x) {
+      const int at = x * 256 + tid, j = at / KV, pos = prefix + __shfl(src, j & 63);
+      if (x * 256 / KV >= cnt) break;
+      const uint8_t* const blk = block(j < cnt ? pos : prefix);
+      if (j < cnt) k[x] = *reinterpret_cast<const u32x4*>(blk + k0 + (int64_t)(pos & (a.pb - 1)) * D * ES + at % KV * 16);
     }
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      if (!move[b]) continue;
-      const int pos = prefix + j0 + b, slot = pos & (a.pb - 1);
-      uint8_t* const blk = a.pool + (int64_t)table[pos >> psh] * a.block_bytes;
-      *reinterpret_cast<u32x4*>(blk + koff + (int64_t)slot * D * ES) = k[b];
-#pragma unroll
-      for (int c = 0; c < C; ++c) *reinterpret_cast<E*>(blk + voff + ((int64_t)c * a.pb + slot) * ES) = v[b][c];
+    for (int x = 0; x < NV; ++x) {
+      const int at = x * 256 + tid, j = at & ((1 << wsh) - 1), ch = at >> wsh, pos = prefix + __shfl(src, j);
+      if (x * 256 >> wsh >= D) break;
+      const bool on = j < cnt && ch < D;
+      const uint8_t* const blk = block(on ? pos : prefix);
+      if (on) v[x] = *reinterpret_cast<const E*>(blk + v0 + ((int64_t)ch * a.pb + (pos & (a.pb - 1))) * ES);
     }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      const int at = x * 256 + tid, j = at / KV, pos = prefix + j0 + j;
+      if (x * 256 / KV >= cnt) break;
+      uint8_t* const blk = block(j < cnt ? pos : prefix);
+      if (j < cnt) *reinterpret_cast<u32x4*>(blk + k0 + (int64_t)(pos & (a.pb - 1)) * D * ES + at % KV * 16) = k[x];
+    }
+#pragma unroll
+    for (int x = 0; x < NV; ++x) {
+      const int at = x * 256 + tid, j = at & ((1 << wsh) - 1), ch = at >> wsh, pos = prefix + j0 + j;
+      if (x * 256 >> wsh >= D) break;
+      const bool on = j < cnt && ch < D;
+      uint8_t* const blk = block(on ? pos : prefix);
+      if (on) *reinterpret_cast<E*>(blk + v0 + ((int64_t)ch * a.pb + (pos & (a.pb - 1))) * ES) = v[x];
+    }
+    if (cnt < B) return;
   }
 }
 
@@ -197,8 +220,7 @@ flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, 
 flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, const int32_t* n_accept,
                                 const int32_t* path, hipStream_t stream) {
   if (list.n <= 0) return FLP_OK;
-  const int per = 256 * 16 / elem_bytes;
-  const dim3 grid((unsigned)list.n, (unsigned)((a.n_kv * head_dim + per - 1) / per));
+  const dim3 grid((unsigned)(list.n * a.n_kv));
   const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, list, n_accept, path); };
   if (elem_bytes == 1)
     head_dim == 64 ? launch(kv_accept_kernel<1, 64>) : launch(kv_accept_kernel<1, 128>);

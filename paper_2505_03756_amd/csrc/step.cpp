@@ -159,7 +159,7 @@ flp_status append8(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_sca
 struct AttnLaunch {
   std::vector<FlpStepSeq> recs;
   bool tiles;                  // attention_step_tiles.hip
-  int32_t row_tiles, row_waves, merge_rows;
+  int32_t row_tiles, row_waves, waves, merge_rows;
   int64_t units;
 };
 
@@ -208,6 +208,7 @@ std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, cons
         l.merge_rows += r.n;
       }
     }
+    l.waves = l.row_tiles == 1 && l.units * n_kv <= 256 ? 8 : 4;
     launches.push_back(std::move(l));
   }
   *part_rows = (size_t)parts;
@@ -260,7 +261,7 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
       at += l.recs.size();
     }
     s = l.tiles ? flp_launch_attn_step_tiles(p->cfg.dtype, a, list, l.units, stream)
-                : flp_launch_attn_step(p->cfg.dtype, p->cfg.head_dim, a, list, l.row_tiles, l.units, stream);
+                : flp_launch_attn_step(p->cfg.dtype, p->cfg.head_dim, a, list, l.row_tiles, l.waves, l.units, stream);
     if (s == FLP_OK) s = flp_launch_attn_step_merge(p->cfg.dtype, p->cfg.head_dim, a, list, stream);
   }
   if (!slot) return s;
