@@ -5,22 +5,23 @@
 // (sm_scale k_scale) q_r . K_k.  A token sees every position of the prefix; of its sequence's new tokens those up to itself, or
 // those whose bit is set in its mask.  A row that sees nothing is zero.
 //
-// One wave owns 16 J rows of one (sequence, kv head) and walks tiles of the context with a running maximum and sum.  K and V go from
+// One wave owns 16 rows of one (sequence, kv head) and walks tiles of the context with a running maximum and sum.  K and V go from
 // memory to registers 16 bytes per lane and are used there for all rows; nothing is staged.  S^T = K Q^T and O^T = V^T W^T with
-// 16x16 instructions: a lane holds one query row (column l % 16) of every row tile and the RUN = 16 bytes / element size consecutive
+// 16x16 instructions: a lane holds one query row (column l % 16) and the RUN = 16 bytes / element size consecutive
 // positions from RUN (l / 16) on, because row m of key tile t is key RUN (m / 4) + 4 t + m % 4; these positions are also its 16-byte
 // run of the transposed V.  Which channels a step of the scores takes is free as long as K and Q agree, so that a lane's 16 bytes of
 // K are one step in 16 bits, two in 8, four (16x16x4) in fp32.
 //
 //   fp32     fp32 instructions throughout.
 //   16 bit   weights in two pieces of the pool's type, the value and its remainder: 16 bits of them in bf16 and 22 in fp16, where one
-//            piece would add an error as large as the rounding of the result.  An infinite V would meet a negative remainder, so the
-//            words of V are looked over first and what is not finite goes another way (below).
+//            piece would add an error as large as the rounding of the result.  An infinite V would meet a negative remainder, so V
+//            is multiplied by zero first, and what is not finite goes another way (below).
 //   8 bit    e4m3 is exact in fp16 and in bf16: K is widened to the type of q, V and the weights to fp16, two pieces as well.
 //
-// A workgroup is four waves (eight in small launches): row tiles x slices of the context, so that waves of different row tiles read the same K and V at about
-// the same time, and slices are merged in LDS.  Long contexts of small launches are cut into pieces over workgroups as well, which
-// a second launch merges in piece order.  Bound by the traffic of K and V up to 32 rows or so per kv head.
+// A workgroup is four waves, eight in small launches.  Where the launch has enough of them they are independent, side by side on row tiles
+// of a (sequence, kv head), which then read the same K and V at about the same time, or on kv heads; otherwise they take slices of the
+// context, merged in LDS.  Contexts of the smallest launches are cut into pieces over workgroups as well, because one CU
+// fetches no more than 64 bytes a nanosecond; a second launch merges them in piece order.
 //
 // Infinities and NaN in V reach the rows that see them and no others: in the tiles where some row does not see everything, and in
 // all tiles of 16-bit V, values that are not finite are replaced by zero, and whether a row sees one is counted with products of
@@ -104,75 +105,51 @@ __device__ __forceinline__ float got(float v, int) { return v; }
 __device__ __forceinline__ float got(h16x8 v, int e) { return (float)v[e]; }
 __device__ __forceinline__ float got(b16x8 v, int e) { return (float)v[e]; }
 
-template <typename S, int D, int J, bool KV8, int W>
-__global__ __launch_bounds__(64 * W, J == 1 ? 2 : 1) void attn_step_kernel(FlpStepArgs a, FlpStepList list) {
+// W waves per workgroup, NL records in the arguments
+template <typename S, int D, bool KV8, int W, int NL>
+__global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, FlpStepList<NL> list) {
   typedef Kind<S, KV8> C;
   typedef typename C::kvec kvec;
   typedef typename C::vvec vvec;
   typedef typename S::storage ST;
   constexpr int RUN = 16 / C::ES, TP = 4 * RUN, NT = RUN / 4, KC = D * C::ES / 64, CT = D / 16, STEPS = C::STEPS;
   constexpr int VE = RUN / STEPS;                      // positions of a lane's run that one step of the second product takes
-  __shared__ f32x4 merge_o[W][CT][J][64];
-  __shared__ float2 merge_ml[W][J][16];
+  constexpr uint32_t ALL = (1u << RUN) - 1;
+  __shared__ f32x4 merge_o[W][CT][64];
+  __shared__ float2 merge_ml[W][16];
 
   const int lane = threadIdx.x & 63, lr = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int u = blockIdx.x / a.n_kv, g = blockIdx.x - u * a.n_kv;
+  // waves side by side on kv heads, within a head on row tiles, and within those on slices of the context
+  const int hw = a.head_waves, rw = a.row_waves, per_head = W / hw, kw = per_head / rw;
+  const int head_groups = (a.n_kv + hw - 1) / hw, u = blockIdx.x / head_groups;
+  const int own_head = (blockIdx.x - u * head_groups) * hw + wave / per_head, in_head = wave % per_head;
+  const int g = own_head < a.n_kv ? own_head : a.n_kv - 1;
   const FlpStepSeq rec = flp_step_record(a, list, u, &FlpStepSeq::unit0);
   const int G = a.n_h / a.n_kv, R = rec.n * G, P = rec.prefix, L = P + rec.n;
-  const int rw = a.row_waves, kw = W / rw;             // waves side by side on row tiles, and on slices of the context
-  const int groups = (R + 16 * J * rw - 1) / (16 * J * rw);      // workgroups that the rows take
+  const int groups = (R + 16 * rw - 1) / (16 * rw);    // workgroups that the rows take
   const int local = u - rec.unit0, piece = local / groups, rgroup = local - piece * groups;
-  const int row0 = (rgroup * rw + wave % rw) * 16 * J, slice = wave / rw;
-  const bool active = row0 < R;
-  const int row_last = row0 + 16 * J < R ? row0 + 16 * J - 1 : R - 1;
+  const int row0 = (rgroup * rw + in_head % rw) * 16, slice = in_head / rw;
+  const bool active = row0 < R && own_head < a.n_kv;
+  const int row_last = row0 + 16 < R ? row0 + 15 : R - 1;
 
-  // tiles of the piece, and those of them that this wave's rows see something of
+  // ---- this lane's place in a tile: its K rows are keys RUN (lr / 4) + 4 t + lr % 4, its run of V starts at position RUN lh
+  const int pb = a.pb, psh = __builtin_ctz(pb), last = (L - 1) / RUN;      // the last run that holds a position of the sequence
+  const int32_t* __restrict__ table = a.tables + (int64_t)rec.seq * a.max_blocks;
+  const auto run_of = [&](int tile, int sel) {         // past the end: the last run again
+    const int r = 4 * tile + sel;
+    return (r < last ? r : last) * RUN;
+  };
+  const auto id = [&](int tile, int sel) { return table[run_of(tile, sel) >> psh]; };
+
+  // ---- tiles of the piece, and those of them that this wave's rows see something of
   const int n_tiles = (L + TP - 1) / TP;
   const int lo = (int)((int64_t)n_tiles * piece / rec.pieces);
   int hi = (int)((int64_t)n_tiles * (piece + 1) / rec.pieces);
   const int sees = a.mask ? L : P + row_last / G + 1;  // positions that the wave's rows see together
   if (hi > (sees + TP - 1) / TP) hi = (sees + TP - 1) / TP;
   const int all_see = a.mask ? P : P + row0 / G + 1;   // positions that each of them sees
-  const float c = a.scale_log2e * (KV8 ? a.k_scale[g] : 1.f);
 
-  // ---- the rows: token and head, the queries, what of the new tokens they see
-  int64_t rowoff[J];
-  int tok[J];
-  uint64_t bits[J];
-  kvec qf[J][KC * STEPS];
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int r = row0 + 16 * j + lr, rc = r < R ? r : R - 1;
-    tok[j] = rc / G;
-    rowoff[j] = ((int64_t)(rec.t0 + tok[j]) * a.n_h + (g * G + rc - tok[j] * G)) * D;
-    bits[j] = 0;
-    if (a.mask) bits[j] = a.mask[rec.t0 + tok[j]] & (~0ull >> (64 - rec.n));
-    const ST* qp = reinterpret_cast<const ST*>(a.q) + rowoff[j];
-#pragma unroll
-    for (int cc = 0; cc < KC; ++cc) {
-      constexpr int PER = 16 / C::ES;                  // channels of a lane's 16 bytes of K
-      const ST* p = qp + cc * 4 * PER + lh * PER;
-      if constexpr (std::is_same<S, F32>::value) {
-        const u32x4 raw = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) qf[j][cc * STEPS + s] = __uint_as_float(raw[s]);
-      } else {
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) qf[j][cc * STEPS + s] = bits_as<kvec>(*reinterpret_cast<const u32x4*>(p + 8 * s));
-      }
-    }
-  }
-
-  // ---- this lane's place in a tile: its K rows are keys RUN (lr / 4) + 4 t + lr % 4, its run of V starts at position RUN lh
-  const int pb = a.pb, last = (L - 1) / RUN;           // the last run that holds a position of the sequence
-  const int32_t* __restrict__ table = a.tables + (int64_t)rec.seq * a.max_blocks;
-  const int psh = __builtin_ctz(pb);
-  const auto run_of = [&](int tile, int sel) {
-    const int r = 4 * tile + sel;
-    return (r < last ? r : last) * RUN;
-  };
-  const auto id = [&](int tile, int sel) { return table[run_of(tile, sel) >> psh]; };
   u32x4 kr[NT][KC], vr[CT];
   const auto load_k = [&](int tile, int32_t blk) {
     const int slot = (run_of(tile, lr >> 2) & (pb - 1)) + (lr & 3);
@@ -188,60 +165,75 @@ __global__ __launch_bounds__(64 * W, J == 1 ? 2 : 1) void attn_step_kernel(FlpSt
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) vr[ct] = *reinterpret_cast<const u32x4*>(p + (int64_t)16 * ct * pb * C::ES);
   };
-
-  f32x4 O[CT][J];
-  float m[J], l[J];
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    m[j] = -INFINITY;
-    l[j] = 0.f;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) O[ct][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int tile0 = lo + slice;
+  const bool works = active && tile0 < hi;
+  int32_t idk = 0, idv = 0;                            // blocks of the tile that is requested next
+  if (works) {
+    const int32_t k0 = id(tile0, lr >> 2), v0 = id(tile0, lh);
+    idk = id(tile0 + kw, lr >> 2);
+    idv = id(tile0 + kw, lh);
+    load_k(tile0, k0);
+    load_v(tile0, v0);
   }
+
+  // ---- the rows: token and head, the queries, what of the new tokens they see
+  const int r = row0 + lr, rc = r < R ? r : R - 1, tok = rc / G;
+  const int64_t rowoff = ((int64_t)(rec.t0 + tok) * a.n_h + (g * G + rc - tok * G)) * D;
+  const uint64_t bits = a.mask ? a.mask[rec.t0 + tok] & (~0ull >> (64 - rec.n)) : 0;
+  const float c = a.scale_log2e * (KV8 ? a.k_scale[g] : 1.f);
+  kvec qf[KC * STEPS];
+#pragma unroll
+  for (int cc = 0; cc < KC; ++cc) {
+    constexpr int PER = 16 / C::ES;                    // channels of a lane's 16 bytes of K
+    const ST* p = reinterpret_cast<const ST*>(a.q) + rowoff + cc * 4 * PER + lh * PER;
+    if constexpr (std::is_same<S, F32>::value) {
+      const u32x4 raw = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) qf[cc * STEPS + s] = __uint_as_float(raw[s]);
+    } else {
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) qf[cc * STEPS + s] = bits_as<kvec>(*reinterpret_cast<const u32x4*>(p + 8 * s));
+    }
+  }
+
+  f32x4 O[CT];
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) O[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // V with values that are not finite: they are replaced by zero, and which sums they would have gone into is kept, a byte per four
   // channels of a row, in the wave's part of the merge's LDS (bit e of vis: position e of the lane's run).  NaN counts as both infinities.
   bool flagged = false;
-  uint8_t* const flags = reinterpret_cast<uint8_t*>(&merge_o[wave][0][0][0]) + lane;
-  const auto not_finite = [&](const uint32_t (&vis)[J]) {
+  uint8_t* const flags = reinterpret_cast<uint8_t*>(&merge_o[wave][0][0]) + lane;
+  const auto not_finite = [&](uint32_t vis) __attribute__((always_inline)) {
     if (!flagged)
 #pragma unroll 1
-      for (int x = 0; x < CT * J; ++x) flags[64 * x] = 0;
+      for (int x = 0; x < CT; ++x) flags[64 * x] = 0;
     flagged = true;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      uint32_t f[J];
-#pragma unroll
-      for (int j = 0; j < J; ++j) f[j] = 0;
+      uint32_t f = 0;
 #pragma unroll
       for (int sign = 0; sign < (KV8 ? 1 : 2); ++sign) {             // e4m3 has no infinities
-        f32x4 n[J];
-#pragma unroll
-        for (int j = 0; j < J; ++j) n[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x4 n = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
           const vvec x = C::v(vr[ct], s);
-          vvec is;
+          uint32_t b = vis;
+          asm volatile("" : "+v"(b));                  // here each time: kept for all channels the indicators would cost registers
+          vvec is, seen;
 #pragma unroll
           for (int e = 0; e < VE; ++e) {
-            const float v = got(x, e);
-            put(is, e, v != v || v == (sign ? -INFINITY : INFINITY) ? 1.f : 0.f);
+            const float y = got(x, e);
+            put(is, e, y != y || y == (sign ? -INFINITY : INFINITY) ? 1.f : 0.f);
+            put(seen, e, (b >> (VE * s + e)) & 1 ? 1.f : 0.f);
           }
-#pragma unroll
-          for (int j = 0; j < J; ++j) {
-            vvec seen;
-#pragma unroll
-            for (int e = 0; e < VE; ++e) put(seen, e, (vis[j] >> (VE * s + e)) & 1 ? 1.f : 0.f);
-            n[j] = mma(is, seen, n[j]);
-          }
+          n = mma(is, seen, n);
         }
 #pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f[j] |= n[j][i] > 0.f ? (KV8 ? 0x11u : sign ? 0x10u : 1u) << i : 0u;
+        for (int i = 0; i < 4; ++i) f |= n[i] > 0.f ? (KV8 ? 0x11u : sign ? 0x10u : 1u) << i : 0u;
       }
-#pragma unroll
-      for (int j = 0; j < J; ++j) flags[64 * (ct * J + j)] |= (uint8_t)f[j];
+      flags[64 * ct] |= (uint8_t)f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {                    // the high bit of each such value, spread over it
         const uint32_t o = C::odd(vr[ct][w]);
@@ -251,48 +243,43 @@ __global__ __launch_bounds__(64 * W, J == 1 ? 2 : 1) void attn_step_kernel(FlpSt
     }
   };
 
-  const auto step = [&](int tile, int next, int32_t next_k, int32_t next_v) {
-    f32x4 s[NT][J];
+  const auto step = [&](int tile) __attribute__((always_inline)) {
+    const int next = tile + kw;
+    const bool more = next < hi;
+    const int32_t next_k = idk, next_v = idv;
+    if (more) {
+      idk = id(next + kw, lr >> 2);
+      idv = id(next + kw, lh);
+    }
+    f32x4 s[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-#pragma unroll
-      for (int j = 0; j < J; ++j) s[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int cc = 0; cc < KC; ++cc)
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-          const kvec kv = C::k(kr[t][cc], st);
-#pragma unroll
-          for (int j = 0; j < J; ++j) s[t][j] = mma(kv, qf[j][cc * STEPS + st], s[t][j]);
-        }
+        for (int st = 0; st < STEPS; ++st) s[t] = mma(C::k(kr[t][cc], st), qf[cc * STEPS + st], s[t]);
     }
-    if (J == 1) {                                      // on their way during the rest of the step
-      __builtin_amdgcn_sched_barrier(0);
-      load_k(next, next_k);
-    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) load_k(next, next_k);                 // on their way during the rest of the step
     __builtin_amdgcn_sched_barrier(0);
 
     const int p0 = TP * tile + RUN * lh;
     const bool careful = TP * tile + TP > all_see;     // some row does not see the whole tile
-    uint32_t vis[J];
-#pragma unroll
-    for (int j = 0; j < J; ++j) vis[j] = (1u << RUN) - 1;
+    uint32_t vis = ALL;
     if (careful) {
-      const auto low = [&](int n) { return n <= 0 ? 0u : n >= RUN ? (1u << RUN) - 1 : (1u << n) - 1; };
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        if (a.mask) {
-          const int ahead = p0 - P;                    // which new token the run's first position holds
-          const uint64_t b = ahead >= 64 || ahead <= -64 ? 0 : ahead >= 0 ? bits[j] >> ahead : bits[j] << -ahead;
-          vis[j] = low(P - p0) | ((uint32_t)b & ((1u << RUN) - 1));
-        } else {
-          vis[j] = low(P + tok[j] + 1 - p0);
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[t][j][i] = (vis[j] >> (4 * t + i)) & 1 ? s[t][j][i] : -INFINITY;
+      const auto low = [&](int n) { return n <= 0 ? 0u : n >= RUN ? ALL : (1u << n) - 1; };
+      if (a.mask) {
+        const int ahead = p0 - P;                      // which new token the run's first position holds
+        const uint64_t x = ahead >= 64 || ahead <= -64 ? 0 : ahead >= 0 ? bits >> ahead : bits << -ahead;
+        vis = low(P - p0) | ((uint32_t)x & ALL);
+      } else {
+        vis = low(P + tok + 1 - p0);
       }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[t][i] = (vis >> (4 * t + i)) & 1 ? s[t][i] : -INFINITY;
       const uint32_t there = low(L - p0);              // slots past the end hold arbitrary bits
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
@@ -304,62 +291,59 @@ __global__ __launch_bounds__(64 * W, J == 1 ? 2 : 1) void attn_step_kernel(FlpSt
         for (int ct = 0; ct < CT; ++ct) vr[ct][w] &= keep;
       }
     }
+
     // The running maximum is raised only when a row has outgrown it by 2^8: until then weights are relative to the old one
-    float tm[J];
-    bool grew = false;
+    float tm = s[0][0];
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      tm[j] = s[0][j][0];
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tm[j] = fmaxf(tm[j], s[t][j][i]);
-      grew = grew || (tm[j] - m[j]) * c > 8.f;
-    }
-    if (__builtin_amdgcn_ballot_w64(grew)) {
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        tm[j] = fmaxf(tm[j], __shfl_xor(tm[j], 16));
-        tm[j] = fmaxf(tm[j], __shfl_xor(tm[j], 32));
-        const float mn = fmaxf(m[j], tm[j]);
-        const float alpha = mn == m[j] ? 1.f : __builtin_amdgcn_exp2f((m[j] - mn) * c);
-        m[j] = mn;
-        l[j] *= alpha;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) O[ct][j][i] *= alpha;
-      }
-    }
-    vvec w[J][STEPS][C::PIECES];
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const float mc = m[j] == -INFINITY ? 0.f : m[j] * c;
-      float sum = 0.f;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = __builtin_amdgcn_exp2f(fmaf(s[t][j][i], c, -mc));
-          sum += x;
-          const int e = 4 * t + i;
-          put(w[j][e / VE][0], e % VE, x);
-          if constexpr (C::PIECES == 2) put(w[j][e / VE][1], e % VE, x - got(w[j][e / VE][0], e % VE));
-        }
-      l[j] += sum;
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if (careful || !KV8) {
-      uint32_t any = 0;
+      for (int i = 0; i < 4; ++i) tm = fmaxf(tm, s[t][i]);
+    if (__builtin_amdgcn_ballot_w64((tm - m) * c > 8.f)) {
+      tm = fmaxf(tm, __shfl_xor(tm, 16));
+      tm = fmaxf(tm, __shfl_xor(tm, 32));
+      const float mn = fmaxf(m, tm);
+      const float alpha = mn == m ? 1.f : __builtin_amdgcn_exp2f((m - mn) * c);
+      m = mn;
+      l *= alpha;
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) any |= C::odd(vr[ct][w]);
-      if (__builtin_amdgcn_ballot_w64(any != 0)) not_finite(vis);
+        for (int i = 0; i < 4; ++i) O[ct][i] *= alpha;
     }
-    if (J > 1) {                                       // more rows: the scores' registers are free only now
-      load_k(next, next_k);
-      __builtin_amdgcn_sched_barrier(0);
+    vvec w[STEPS][C::PIECES];
+    const float mc = m == -INFINITY ? 0.f : m * c;     // nothing seen yet: weights 0
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][i], c, -mc));
+        sum += x;
+        const int e = 4 * t + i;
+        put(w[e / VE][0], e % VE, x);
+        if constexpr (C::PIECES == 2) put(w[e / VE][1], e % VE, x - got(w[e / VE][0], e % VE));
+      }
+    l += sum;
+    __builtin_amdgcn_sched_barrier(0);
+    if (careful || !KV8) {
+      bool any = false;
+      if constexpr (C::ES == 2) {                      // zero times V: the matrix cores have the time, the vector units have not
+        f32x4 z[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        vvec zero = {};
+        asm volatile("" : "+v"(zero));                 // or the products are folded away
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) z[ct & 1] = mma(C::v(vr[ct], 0), zero, z[ct & 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) any = any || z[0][i] != z[0][i] || z[1][i] != z[1][i];
+      } else {
+        uint32_t odd = 0;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) odd |= C::odd(vr[ct][x]);
+        any = odd != 0;
+      }
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(any) != 0, 0)) not_finite(vis);
     }
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
@@ -367,125 +351,83 @@ __global__ __launch_bounds__(64 * W, J == 1 ? 2 : 1) void attn_step_kernel(FlpSt
       for (int st = 0; st < STEPS; ++st) {
         const vvec v = C::v(vr[ct], st);
 #pragma unroll
-        for (int pc = C::PIECES - 1; pc >= 0; --pc)
-#pragma unroll
-          for (int j = 0; j < J; ++j) O[ct][j] = mma(v, w[j][st][pc], O[ct][j]);
+        for (int pc = C::PIECES - 1; pc >= 0; --pc) O[ct] = mma(v, w[st][pc], O[ct]);
       }
     __builtin_amdgcn_sched_barrier(0);
-    load_v(next, next_v);
+    if (more) load_v(next, next_v);
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  if (active && lo + slice < hi) {
-    int tile = lo + slice;
-    int32_t idk = id(tile, lr >> 2), idv = id(tile, lh);
-    load_k(tile, idk);
-    load_v(tile, idv);
-    int32_t nk = id(tile + kw, lr >> 2), nv = id(tile + kw, lh);
-    for (; tile < hi; tile += kw) {                    // loads past the end: the last run again, not used
-      idk = nk;
-      idv = nv;
-      nk = id(tile + 2 * kw, lr >> 2);
-      nv = id(tile + 2 * kw, lh);
-      step(tile, tile + kw, idk, idv);
-    }
-  }
+  if (works)
+    for (int tile = tile0; tile < hi; tile += kw) step(tile);
   if (flagged)
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const uint32_t f = flags[64 * (ct * J + j)];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if ((f >> i) & 1) O[ct][j][i] += INFINITY;
-          if ((f >> (4 + i)) & 1) O[ct][j][i] -= INFINITY;
-        }
-      }
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    l[j] += __shfl_xor(l[j], 16);
-    l[j] += __shfl_xor(l[j], 32);
-  }
-
-  // ---- slices of the context, then the result or the piece's share of it.  Lane (row lr, quarter lh): channels 16 ct + 4 lh ..
-  const float vs = KV8 ? a.v_scale[g] : 1.f;
-  float M[J], Lsum[J], factor[J][W];
-  if (kw > 1) {
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      if (lh == 0) merge_ml[wave][j][lr] = make_float2(m[j], l[j]);
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) merge_o[wave][ct][j][lane] = O[ct][j];
-    }
-    __syncthreads();
-  }
-  if (!active) return;
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    M[j] = m[j];
-    Lsum[j] = l[j];
-    if (kw > 1) {
-      const int first = wave % rw;
-      float mm[W], ll[W];
-      M[j] = -INFINITY;
-      Lsum[j] = 0.f;
-#pragma unroll
-      for (int x = 0; x < W; ++x) {
-        const float2 v = merge_ml[(first + x * rw) & (W - 1)][j][lr];
-        mm[x] = x < kw ? v.x : -INFINITY;
-        ll[x] = v.y;
-        M[j] = fmaxf(M[j], mm[x]);
-      }
-#pragma unroll
-      for (int x = 0; x < W; ++x) {
-        factor[j][x] = mm[x] == -INFINITY ? 0.f : mm[x] == M[j] ? 1.f : __builtin_amdgcn_exp2f((mm[x] - M[j]) * c);
-        if (x < kw) Lsum[j] += factor[j][x] == 0.f ? (ll[x] != ll[x] ? ll[x] : 0.f) : ll[x] * factor[j][x];
-      }
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int r = row0 + 16 * j + lr;
-    const bool nothing = a.mask && P == 0 && bits[j] == 0;
-    const float inv = nothing ? 0.f : vs / Lsum[j];
-    const int64_t prow = (int64_t)rec.part0 + (int64_t)tok[j] * rec.pieces + piece;
-    float* const pp = a.partials + (prow * a.n_h + (rowoff[j] / D - (int64_t)(rec.t0 + tok[j]) * a.n_h)) * (D + 2);
-    if (r < R && rec.pieces > 1 && lh == 0 && slice == 0) *reinterpret_cast<float2*>(pp) = make_float2(M[j] * c, Lsum[j]);
-#pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      if (kw > 1 && (ct & (kw - 1)) != slice) continue;
-      f32x4 o = O[ct][j];
-      if (kw > 1) {
-        o = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int first = wave % rw;
+      const uint32_t f = flags[64 * ct];
 #pragma unroll
-        for (int x = 0; x < W; ++x)
-          if (x < kw && factor[j][x] != 0.f) {
-            const f32x4 v = merge_o[(first + x * rw) & (W - 1)][ct][j][lane];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], factor[j][x], o[i]);
-          }
+      for (int i = 0; i < 4; ++i) {
+        if ((f >> i) & 1) O[ct][i] += INFINITY;
+        if ((f >> (4 + i)) & 1) O[ct][i] -= INFINITY;
       }
-      if (r >= R) continue;
-      if (rec.pieces > 1) {
-        float2* const d2 = reinterpret_cast<float2*>(pp + 2 + 16 * ct + 4 * lh);
-        d2[0] = make_float2(o[0] * vs, o[1] * vs);
-        d2[1] = make_float2(o[2] * vs, o[3] * vs);
-        continue;
-      }
-      ST* const op = reinterpret_cast<ST*>(a.out) + rowoff[j] + 16 * ct + 4 * lh;
-      ST e[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) e[i] = nothing ? S::from_float(0.f) : S::from_float(o[i] * inv);
-      __builtin_memcpy(__builtin_assume_aligned(op, 4 * sizeof(ST)), e, sizeof(e));
     }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+
+  // ---- slices of the context, then the result or the piece's share of it.  Lane (row lr, quarter lh): channels 16 ct + 4 lh ..; a wave
+  //      takes every kw-th channel tile of its rows.  In a loop that is not unrolled: small calls wait for the code as well
+  const float vs = KV8 ? a.v_scale[g] : 1.f;
+  if (lh == 0) merge_ml[wave][lr] = make_float2(m, l);
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) merge_o[wave][ct][lane] = O[ct];
+  __syncthreads();
+  if (!active) return;
+  const int first = wave - slice * rw;
+  float M = -INFINITY, total = 0.f, factor[W];
+  float2 ml[W];
+#pragma unroll
+  for (int x = 0; x < W; ++x) {
+    ml[x] = merge_ml[(first + x * rw) & (W - 1)][lr];
+    if (x >= kw) ml[x] = make_float2(-INFINITY, 0.f);
+    M = fmaxf(M, ml[x].x);
+  }
+#pragma unroll
+  for (int x = 0; x < W; ++x) {
+    factor[x] = ml[x].x == -INFINITY ? 0.f : ml[x].x == M ? 1.f : __builtin_amdgcn_exp2f((ml[x].x - M) * c);
+    total = fmaf(ml[x].y, factor[x], total);
+  }
+  const bool nothing = a.mask && P == 0 && bits == 0;
+  const float inv = vs / total;
+  const int64_t prow = (int64_t)rec.part0 + (int64_t)tok * rec.pieces + piece;
+  float* const pp = a.partials + (prow * a.n_h + (g * G + (rc - tok * G))) * (D + 2);
+  if (r < R && rec.pieces > 1 && lh == 0 && slice == 0) *reinterpret_cast<float2*>(pp) = make_float2(M * c, total);
+#pragma unroll 1
+  for (int ct = slice; ct < CT; ct += kw) {
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < W; ++x) {
+      const f32x4 v = merge_o[(first + x * rw) & (W - 1)][ct][lane];
+      if (x < kw)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], factor[x], o[i]);
+    }
+    if (r >= R) continue;
+    if (rec.pieces > 1) {
+      float2* const d2 = reinterpret_cast<float2*>(pp + 2 + 16 * ct + 4 * lh);
+      d2[0] = make_float2(o[0] * vs, o[1] * vs);
+      d2[1] = make_float2(o[2] * vs, o[3] * vs);
+      continue;
+    }
+    ST* const op = reinterpret_cast<ST*>(a.out) + rowoff + 16 * ct + 4 * lh;
+    ST e[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = S::from_float(nothing ? 0.f : o[i] * inv);
+    __builtin_memcpy(__builtin_assume_aligned(op, 4 * sizeof(ST)), e, sizeof(e));
   }
 }
 
 // The pieces of a (token, head) row, at most 64, in piece order: a wave per row, lane i piece i's maximum and sum, every lane its channels
-template <typename S, int D>
-__global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, FlpStepList list) {
+template <typename S, int D, int NL>
+__global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, FlpStepList<NL> list) {
   typedef typename S::storage ST;
   constexpr int CPL = D / 64;
   typedef float chan __attribute__((ext_vector_type(CPL)));
@@ -509,9 +451,9 @@ __global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, Flp
   float M = lane < ns ? mi : -INFINITY;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
-  // a piece that the row sees nothing of has m = -inf, l = 0
+  // a piece that the row sees nothing of has m = -inf, l = 0 and zeros
   const float wi = lane < ns && mi != -INFINITY ? (mi == M ? 1.f : exp2f(mi - M)) : 0.f;
-  float l = lane < ns && (wi != 0.f || li != li) ? (wi != 0.f ? li * wi : li) : 0.f;
+  float l = lane < ns ? li * wi : 0.f;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) l += __shfl_xor(l, off);
   float acc[CPL];
@@ -522,42 +464,38 @@ __global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, Flp
 #pragma unroll
     for (int i = 0; i < B; ++i) {
       const float w = __shfl(wi, (i0 + i) & 63);
-      if (i0 + i < ns && w != 0.f)
+      if (i0 + i < ns)
 #pragma unroll
         for (int x = 0; x < CPL; ++x) acc[x] = fmaf(q[i][x], w, acc[x]);
     }
   }
+  const bool nothing = a.mask && rec.prefix == 0 && (a.mask[rec.t0 + tok] & (~0ull >> (64 - rec.n))) == 0;
   const float inv = 1.f / l;
   ST* op = reinterpret_cast<ST*>(a.out) + ((int64_t)(rec.t0 + tok) * a.n_h + h) * D + CPL * lane;
 #pragma unroll
-  for (int x = 0; x < CPL; ++x) op[x] = S::from_float(acc[x] * inv);
+  for (int x = 0; x < CPL; ++x) op[x] = S::from_float(nothing ? 0.f : acc[x] * inv);
 }
 
-template <typename S, int D, bool KV8>
-void launch_rows(const FlpStepArgs& a, const FlpStepList& list, int row_tiles, int waves, unsigned grid, hipStream_t stream) {
-  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), 0, stream, a, list); };
-  if (row_tiles == 1)
-    waves == 8 ? launch(attn_step_kernel<S, D, 1, KV8, 8>) : launch(attn_step_kernel<S, D, 1, KV8, 4>);
-  else if (row_tiles == 2 || std::is_same<S, F32>::value)
-    launch(attn_step_kernel<S, D, 2, KV8, 4>);
-  else if constexpr (!std::is_same<S, F32>::value)
-    launch(attn_step_kernel<S, D, 4, KV8, 4>);
-}
 template <typename S, int D>
-void launch_kind(const FlpStepArgs& a, const FlpStepList& list, int row_tiles, int waves, unsigned grid, hipStream_t stream) {
-  if constexpr (!std::is_same<S, F32>::value)
-    if (a.k_scale) return launch_rows<S, D, true>(a, list, row_tiles, waves, grid, stream);
-  launch_rows<S, D, false>(a, list, row_tiles, waves, grid, stream);
+void launch_kind(const FlpStepArgs& a, const FlpStepSeq* recs, int waves, unsigned grid, hipStream_t stream) {
+  flp_with_records(a, recs, [&](const auto& list) {
+    constexpr int NL = sizeof(list.seq) / sizeof(FlpStepSeq);
+    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), 0, stream, a, list); };
+    if constexpr (!std::is_same<S, F32>::value)
+      if (a.k_scale)
+        return waves == 8 ? launch(attn_step_kernel<S, D, true, 8, NL>) : launch(attn_step_kernel<S, D, true, 4, NL>);
+    waves == 8 ? launch(attn_step_kernel<S, D, false, 8, NL>) : launch(attn_step_kernel<S, D, false, 4, NL>);
+  });
 }
 
 }  // namespace
 
-flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles, int32_t waves,
-                                int64_t n_units, hipStream_t stream) {
+flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepSeq* inline_recs, int32_t waves, int64_t n_units,
+                                hipStream_t stream) {
   if (n_units <= 0) return FLP_OK;
-  const unsigned grid = (unsigned)(n_units * a.n_kv);
+  const unsigned grid = (unsigned)(n_units * ((a.n_kv + a.head_waves - 1) / a.head_waves));
   const auto launch = [&](auto kind64, auto kind128) {
-    head_dim == 64 ? kind64(a, list, row_tiles, waves, grid, stream) : kind128(a, list, row_tiles, waves, grid, stream);
+    head_dim == 64 ? kind64(a, inline_recs, waves, grid, stream) : kind128(a, inline_recs, waves, grid, stream);
   };
   if (dtype == FLP_F32)
     launch(launch_kind<F32, 64>, launch_kind<F32, 128>);
@@ -569,17 +507,20 @@ flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, c
   return FLP_OK;
 }
 
-flp_status flp_launch_attn_step_merge(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, hipStream_t stream) {
+flp_status flp_launch_attn_step_merge(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepSeq* inline_recs, hipStream_t stream) {
   if (a.merge_rows <= 0) return FLP_OK;
-  const bool d64 = head_dim == 64;
-  const dim3 mgrid((unsigned)(((int64_t)a.merge_rows * a.n_h + 3) / 4));
-  const auto merge = [&](auto kernel) { hipLaunchKernelGGL(kernel, mgrid, dim3(256), 0, stream, a, list); };
-  if (dtype == FLP_F32)
-    d64 ? merge(attn_step_merge_kernel<F32, 64>) : merge(attn_step_merge_kernel<F32, 128>);
-  else if (dtype == FLP_F16)
-    d64 ? merge(attn_step_merge_kernel<F16, 64>) : merge(attn_step_merge_kernel<F16, 128>);
-  else
-    d64 ? merge(attn_step_merge_kernel<BF16, 64>) : merge(attn_step_merge_kernel<BF16, 128>);
+  const dim3 grid((unsigned)(((int64_t)a.merge_rows * a.n_h + 3) / 4));
+  flp_with_records(a, inline_recs, [&](const auto& list) {
+    constexpr int NL = sizeof(list.seq) / sizeof(FlpStepSeq);
+    const bool d64 = head_dim == 64;
+    const auto merge = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, list); };
+    if (dtype == FLP_F32)
+      d64 ? merge(attn_step_merge_kernel<F32, 64, NL>) : merge(attn_step_merge_kernel<F32, 128, NL>);
+    else if (dtype == FLP_F16)
+      d64 ? merge(attn_step_merge_kernel<F16, 64, NL>) : merge(attn_step_merge_kernel<F16, 128, NL>);
+    else
+      d64 ? merge(attn_step_merge_kernel<BF16, 64, NL>) : merge(attn_step_merge_kernel<BF16, 128, NL>);
+  });
   FLP_TRY_HIP(hipGetLastError());
   return FLP_OK;
 }

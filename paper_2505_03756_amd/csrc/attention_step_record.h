@@ -6,7 +6,8 @@
 
 // The last record whose `first` (unit0, or merge0) is not behind `at`, in scalar registers; `at` is the same for the whole wave.  Records in the
 // launch's arguments are read there, a single one together with the other arguments.
-__device__ __forceinline__ FlpStepSeq flp_step_record(const FlpStepArgs& a, const FlpStepList& list, int at, int32_t FlpStepSeq::*first) {
+template <int N>
+__device__ __forceinline__ FlpStepSeq flp_step_record(const FlpStepArgs& a, const FlpStepList<N>& list, int at, int32_t FlpStepSeq::*first) {
   if (a.n_recs == 1) return list.seq[0];
   const auto search = [&](auto recs) {
     int found = -1;
@@ -27,4 +28,19 @@ __device__ __forceinline__ FlpStepSeq flp_step_record(const FlpStepArgs& a, cons
   };
   if (a.recs) return search([&](int i) -> const FlpStepSeq& { return a.recs[i]; });
   return search([&](int i) -> const FlpStepSeq& { return list.seq[i]; });
+}
+
+// launch(list): the kernel with its records in a list as short as they allow
+template <typename F>
+void flp_with_records(const FlpStepArgs& a, const FlpStepSeq* inline_recs, F launch) {
+  const int n = a.recs ? 0 : a.n_recs;
+  if (n <= kShortList) {
+    FlpStepList<kShortList> list;
+    for (int i = 0; i < n; ++i) list.seq[i] = inline_recs[i];
+    launch(list);
+  } else {
+    FlpStepList<kStepInline> list;
+    for (int i = 0; i < n; ++i) list.seq[i] = inline_recs[i];
+    launch(list);
+  }
 }

@@ -46,8 +46,8 @@ __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi) {
   return w;
 }
 
-template <typename M, bool KV8>
-__global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, FlpStepList list) {
+template <typename M, bool KV8, int NL>
+__global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, FlpStepList<NL> list) {
   typedef typename M::vec vec;                                       // scores
   typedef typename std::conditional<KV8, MF16, M>::type MV;          // second product
   typedef typename MV::vec wvec;
@@ -445,15 +445,18 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
 
 }  // namespace
 
-flp_status flp_launch_attn_step_tiles(int dtype, const FlpStepArgs& a, const FlpStepList& list, int64_t n_units, hipStream_t stream) {
+flp_status flp_launch_attn_step_tiles(int dtype, const FlpStepArgs& a, const FlpStepSeq* inline_recs, int64_t n_units, hipStream_t stream) {
   if (n_units <= 0) return FLP_OK;
-  const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(n_units * a.n_kv)), dim3(512), 0, stream, a, list);
-  };
-  if (dtype == FLP_F16)
-    a.k_scale ? launch(attn_step_tiles_kernel<MF16, true>) : launch(attn_step_tiles_kernel<MF16, false>);
-  else
-    a.k_scale ? launch(attn_step_tiles_kernel<MBF16, true>) : launch(attn_step_tiles_kernel<MBF16, false>);
+  flp_with_records(a, inline_recs, [&](const auto& list) {
+    constexpr int NL = sizeof(list.seq) / sizeof(FlpStepSeq);
+    const auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(n_units * a.n_kv)), dim3(512), 0, stream, a, list);
+    };
+    if (dtype == FLP_F16)
+      a.k_scale ? launch(attn_step_tiles_kernel<MF16, true, NL>) : launch(attn_step_tiles_kernel<MF16, false, NL>);
+    else
+      a.k_scale ? launch(attn_step_tiles_kernel<MBF16, true, NL>) : launch(attn_step_tiles_kernel<MBF16, false, NL>);
+  });
   FLP_TRY_HIP(hipGetLastError());
   return FLP_OK;
 }

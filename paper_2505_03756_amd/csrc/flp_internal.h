@@ -198,12 +198,13 @@ constexpr int kMfmaMaxBlocks = 4096;       // longest context of the matrix-core
 
 // ---- the 8-bit cache, drafted trees and accepted paths (step.cpp, attention_step.hip, kv8.hip)
 // The append and the accept launches find their sequences in their own arguments: sequences seq0 .. seq0 + n - 1 of the batch, the new
-// tokens t0[i] .. t0[i + 1] - 1 each, unit0[i]: the first of the append's units that belong to it.  A batch of more takes
-// several launches.
-constexpr int kListSeqs = 300;
+// tokens t0[i] .. t0[i + 1] - 1 each, unit0[i]: the first of the append's units that belong to it.  A batch of more than kListSeqs takes
+// several launches.  Arguments cost their copy (1.6 us for 3 KB), so kernels have a short list and a long one.
+constexpr int kListSeqs = 300, kShortList = 8;
+template <int N>
 struct FlpSeqList {
   int32_t seq0, n;
-  int32_t t0[kListSeqs + 1], prefix[kListSeqs], unit0[kListSeqs];
+  int32_t t0[N + 1], prefix[N], unit0[N];
 };
 // The attention launches have one record per sequence with new tokens: `unit0` is the first of the launch's workgroup units that
 // belong to it.  Up to kStepInline records travel in the launch's own arguments, more of them through a staging slot.
@@ -214,8 +215,9 @@ struct FlpStepSeq {
   int32_t pieces, part0, merge0;   // pieces of the context, first row of the partials, first row of the merge launch
 };
 constexpr int kStepInline = 96;
+template <int N>
 struct FlpStepList {
-  FlpStepSeq seq[kStepInline];
+  FlpStepSeq seq[N];
 };
 struct FlpStepArgs {
   uint8_t* pool;
@@ -225,7 +227,7 @@ struct FlpStepArgs {
   int32_t n_h, n_kv;
   int32_t pb;                  // positions per block of this cache: 16, 32 or 64
   int32_t n_recs, merge_rows;
-  int32_t row_waves;           // attention: waves of a workgroup side by side on row tiles (1, 2 or 4); the others take slices of the context
+  int32_t head_waves, row_waves;   // attention: waves of a workgroup side by side on kv heads and on row tiles (1, or one of them 4)
   float scale_log2e;
   const FlpStepSeq* recs;      // null: in the launch's arguments
   const void* q;
@@ -237,18 +239,18 @@ struct FlpStepArgs {
   const float* v_scale;
   float* partials;             // [piece rows][n_h][head_dim + 2] as in FlpAttnArgs
 };
-// row_tiles (1, 2 or 4): tiles of 16 query rows per wave; waves of a workgroup: 4, with one row tile also 8
-flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, int32_t row_tiles, int32_t waves,
-                                int64_t n_units, hipStream_t stream);
+// inline_recs: the records in host memory where a.recs is null; units of 16 row_waves rows; waves of a workgroup: 4, or 8
+flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepSeq* inline_recs, int32_t waves, int64_t n_units,
+                                hipStream_t stream);
 // many query rows per kv head: 16-bit types, head_dim 128, contexts of up to kMfmaMaxBlocks blocks; units of kMfmaRowsPerItem rows
-flp_status flp_launch_attn_step_tiles(int dtype, const FlpStepArgs& a, const FlpStepList& list, int64_t n_units, hipStream_t stream);
+flp_status flp_launch_attn_step_tiles(int dtype, const FlpStepArgs& a, const FlpStepSeq* inline_recs, int64_t n_units, hipStream_t stream);
 // the pieces of a launch of either kind that has merge rows
-flp_status flp_launch_attn_step_merge(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepList& list, hipStream_t stream);
+flp_status flp_launch_attn_step_merge(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepSeq* inline_recs, hipStream_t stream);
 constexpr int kAppend8Slots = 32;      // a unit of the 8-bit append: the slots of one such run of positions
-flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, int32_t n_units,
+flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpSeqList<kListSeqs>& list, int32_t n_units,
                                  hipStream_t stream);
-flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, const int32_t* n_accept,
-                                const int32_t* path, hipStream_t stream);
+flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpSeqList<kListSeqs>& list,
+                                const int32_t* n_accept, const int32_t* path, hipStream_t stream);
 
 struct FlpLoraArgs {
   const uint8_t* pool;

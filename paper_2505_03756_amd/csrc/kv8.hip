@@ -23,8 +23,8 @@ __device__ __forceinline__ float quotient(float x, float s, float r) {
 // way together.  K: a thread owns 8 channels of 16 slots.  V: a thread owns 4 channels and turns their 32 slots into their 32-byte runs of
 // the transposed V, whole sectors.  A unit that covers part of its run (the ends of a sequence's new tokens) merges its slots into the
 // 16-byte words already there, which belong to this sequence alone; units of one or two slots (a decode batch) store single bytes.
-template <typename S, int D>
-__global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqList list) {
+template <typename S, int D, int N>
+__global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqList<N> list) {
   typedef typename S::storage ST;
   constexpr int SL = kAppend8Slots;
   const int row = a.n_kv * D, u = blockIdx.x;
@@ -136,8 +136,8 @@ __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqLi
 // together, then 32 places of the path at a time are read, K 16 bytes and V an element per access with neighbouring threads on
 // neighbouring places of a channel, and stored behind a barrier.  A place is never behind the token that comes to it, so what is
 // stored for these places is not read for later ones.
-template <int ES, int D>
-__global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpSeqList list, const int32_t* __restrict__ n_accept,
+template <int ES, int D, int N>
+__global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpSeqList<N> list, const int32_t* __restrict__ n_accept,
                                                         const int32_t* __restrict__ path) {
   typedef typename std::conditional<ES == 4, uint32_t, typename std::conditional<ES == 2, uint16_t, uint8_t>::type>::type E;
   constexpr int B = 32, KV = D * ES / 16;              // places at a time; 16-byte pieces of a K row
@@ -202,32 +202,54 @@ __global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpSeqLis
   }
 }
 
+// launch(list): the kernel with its sequences in a list as short as they allow
+template <typename F>
+void with_list(const FlpSeqList<kListSeqs>& list, F launch) {
+  if (list.n > kShortList) return launch(list);
+  FlpSeqList<kShortList> few;
+  few.seq0 = list.seq0;
+  few.n = list.n;
+  for (int i = 0; i < list.n; ++i) {
+    few.t0[i] = list.t0[i];
+    few.prefix[i] = list.prefix[i];
+    few.unit0[i] = list.unit0[i];
+  }
+  few.t0[list.n] = list.t0[list.n];
+  launch(few);
+}
+
 }  // namespace
 
-flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, int32_t n_units,
+flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpSeqList<kListSeqs>& list, int32_t n_units,
                                  hipStream_t stream) {
   if (n_units <= 0) return FLP_OK;
   const dim3 grid((unsigned)n_units, 2 * (unsigned)((a.n_kv * head_dim + 1023) / 1024));
-  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, list); };
-  if (dtype == FLP_F16)
-    head_dim == 64 ? launch(kv_append8_kernel<F16, 64>) : launch(kv_append8_kernel<F16, 128>);
-  else
-    head_dim == 64 ? launch(kv_append8_kernel<BF16, 64>) : launch(kv_append8_kernel<BF16, 128>);
+  with_list(list, [&](const auto& l) {
+    constexpr int N = sizeof(l.prefix) / sizeof(int32_t);
+    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, l); };
+    if (dtype == FLP_F16)
+      head_dim == 64 ? launch(kv_append8_kernel<F16, 64, N>) : launch(kv_append8_kernel<F16, 128, N>);
+    else
+      head_dim == 64 ? launch(kv_append8_kernel<BF16, 64, N>) : launch(kv_append8_kernel<BF16, 128, N>);
+  });
   FLP_TRY_HIP(hipGetLastError());
   return FLP_OK;
 }
 
-flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpSeqList& list, const int32_t* n_accept,
-                                const int32_t* path, hipStream_t stream) {
+flp_status flp_launch_kv_accept(int elem_bytes, int head_dim, const FlpStepArgs& a, const FlpSeqList<kListSeqs>& list,
+                                const int32_t* n_accept, const int32_t* path, hipStream_t stream) {
   if (list.n <= 0) return FLP_OK;
   const dim3 grid((unsigned)(list.n * a.n_kv));
-  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, list, n_accept, path); };
-  if (elem_bytes == 1)
-    head_dim == 64 ? launch(kv_accept_kernel<1, 64>) : launch(kv_accept_kernel<1, 128>);
-  else if (elem_bytes == 2)
-    head_dim == 64 ? launch(kv_accept_kernel<2, 64>) : launch(kv_accept_kernel<2, 128>);
-  else
-    head_dim == 64 ? launch(kv_accept_kernel<4, 64>) : launch(kv_accept_kernel<4, 128>);
+  with_list(list, [&](const auto& l) {
+    constexpr int N = sizeof(l.prefix) / sizeof(int32_t);
+    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, l, n_accept, path); };
+    if (elem_bytes == 1)
+      head_dim == 64 ? launch(kv_accept_kernel<1, 64, N>) : launch(kv_accept_kernel<1, 128, N>);
+    else if (elem_bytes == 2)
+      head_dim == 64 ? launch(kv_accept_kernel<2, 64, N>) : launch(kv_accept_kernel<2, 128, N>);
+    else
+      head_dim == 64 ? launch(kv_accept_kernel<4, 64, N>) : launch(kv_accept_kernel<4, 128, N>);
+  });
   FLP_TRY_HIP(hipGetLastError());
   return FLP_OK;
 }

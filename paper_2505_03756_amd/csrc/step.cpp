@@ -102,7 +102,7 @@ FlpStepArgs make_args(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_
   a.n_h = b->n_q_heads;
   a.n_kv = p->cfg.n_kv_heads;
   a.pb = kv8 ? kv8_tokens(p) : p->cfg.block_tokens;
-  a.row_waves = 1;
+  a.head_waves = a.row_waves = 1;
   a.q = b->q;
   a.out = b->out;
   a.k_new = b->k_new;
@@ -130,7 +130,7 @@ flp_status refuse_capture(hipStream_t stream, const char* who) {
 
 // The sequences of one append or accept launch, from sequence `first` of the batch on; returns the units of its append, the runs of
 // kAppend8Slots positions that get new slots
-int64_t seq_list(const flp_attn_batch* b, int32_t first, FlpSeqList* l) {
+int64_t seq_list(const flp_attn_batch* b, int32_t first, FlpSeqList<kListSeqs>* l) {
   l->seq0 = first;
   l->n = std::min(kListSeqs, b->n_seqs - first);
   int64_t units = 0;
@@ -147,7 +147,7 @@ int64_t seq_list(const flp_attn_batch* b, int32_t first, FlpSeqList* l) {
 
 flp_status append8(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, hipStream_t stream) {
   const FlpStepArgs a = make_args(p, b, sc, true);
-  FlpSeqList list;
+  FlpSeqList<kListSeqs> list;
   for (int32_t first = 0; first < b->n_seqs; first += kListSeqs) {
     const int64_t units = seq_list(b, first, &list);   // below 2^31: so are the new tokens
     FLP_TRY(flp_launch_kv_append8(p->cfg.dtype, p->cfg.head_dim, a, list, (int32_t)units, stream));
@@ -159,56 +159,124 @@ flp_status append8(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_sca
 struct AttnLaunch {
   std::vector<FlpStepSeq> recs;
   bool tiles;                  // attention_step_tiles.hip
-  int32_t row_tiles, row_waves, waves, merge_rows;
+  int32_t head_waves, row_waves, waves, merge_rows;
   int64_t units;
 };
 
-// Sequences with many query rows per kv head go to the tiled kernel, the others to the one that reads K and V straight to registers.
-// Contexts are cut into pieces of equal length so that a launch has about kUnits workgroups.
-constexpr int64_t kUnits = 1024, kTileUnits = 512;
-constexpr int kMinPiece = 4, kMinTilePiece = 8, kMaxPieces = 64;
-constexpr int kFewRows = 64;
+constexpr int kMaxPieces = 64;
+constexpr int kWaveSlots = 512, kTileSlots = 256;      // workgroups of four waves, and of the tiled kernel, that the chip holds at once
+
+void cut(AttnLaunch& l, int64_t piece, int n_kv, const int64_t* tiles, const int64_t* groups, int64_t* parts) {
+  l.units = 0;
+  l.merge_rows = 0;
+  for (size_t i = 0; i < l.recs.size(); ++i) {
+    FlpStepSeq& r = l.recs[i];
+    r.pieces = (int32_t)std::min<int64_t>(kMaxPieces, (tiles[i] + piece - 1) / piece);
+    r.unit0 = (int32_t)l.units;
+    l.units += groups[i] * r.pieces;
+    r.part0 = (int32_t)*parts;
+    r.merge0 = l.merge_rows;
+    if (r.pieces > 1) {
+      *parts += (int64_t)r.n * r.pieces;
+      l.merge_rows += r.n;
+    }
+  }
+}
 
 std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, const std::vector<FlpStepSeq>& all, size_t* part_rows) {
   std::vector<AttnLaunch> launches;
-  const int n_kv = p->cfg.n_kv_heads, pb = p->cfg.block_tokens * (p->elem_bytes / elem_bytes);
+  const int n_kv = p->cfg.n_kv_heads, pb = p->cfg.block_tokens * (p->elem_bytes / elem_bytes), run = 64 / elem_bytes;
   const bool tiles_ok = p->elem_bytes == 2 && p->cfg.head_dim == 128;
-  const auto tiled = [&](const FlpStepSeq& r) {
-    return tiles_ok && (int64_t)r.n * G > kFewRows && ((int64_t)r.prefix + r.n + pb - 1) / pb <= kMfmaMaxBlocks;
+  const auto length = [](const FlpStepSeq& r) { return (int64_t)r.prefix + r.n; };
+  const auto over = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+  const auto fits = [&](const FlpStepSeq& r) { return over(length(r), pb) <= kMfmaMaxBlocks; };
+  // 16-row tiles of the queries times tiles of the context, over all kv heads, of the sequences with more than `rows` query rows and of the others
+  const auto work = [&](int rows, int64_t (&w)[2]) {
+    w[0] = w[1] = 0;
+    for (const FlpStepSeq& r : all)
+      w[tiles_ok && fits(r) && (int64_t)r.n * G > rows] += over((int64_t)r.n * G, 16) * over(length(r), run) * n_kv;
   };
+  int64_t w[2];
+  int from = 16;                                       // sequences with more query rows than that go to the tiled kernel
+  work(from, w);
+  if (elem_bytes == 1 || w[1] < 8 * w[0]) work(from = 64, w);
+  if (w[1] <= (elem_bytes == 1 ? 12000 : 6000))
+    from = INT32_MAX;
+  else if (w[1] > 8 * w[0])
+    from = 0;                                          // what little is left comes along
+  const auto tiled = [&](const FlpStepSeq& r) { return tiles_ok && fits(r) && (int64_t)r.n * G > from; };
   int64_t parts = 0;
-  for (int tiles = 1; tiles >= 0; --tiles) {
+  std::vector<int64_t> tiles, groups;
+  for (int t = 1; t >= 0; --t) {
     AttnLaunch l{};
+    l.tiles = t == 1;
     int64_t rows = 0;
     for (const FlpStepSeq& r : all)
-      if (tiled(r) == (tiles == 1)) {
+      if (tiled(r) == l.tiles) {
         l.recs.push_back(r);
         rows = std::max<int64_t>(rows, (int64_t)r.n * G);
       }
     if (l.recs.empty()) continue;
-    l.tiles = tiles == 1;
-    l.row_tiles = rows <= 16 ? 1 : rows <= 32 || elem_bytes == 4 ? 2 : 4;      // fp32: four tiles do not fit the registers
-    l.row_waves = rows <= 16 * l.row_tiles ? 1 : rows <= 32 * l.row_tiles ? 2 : 4;
-    const int tile = l.tiles ? 64 : 64 / elem_bytes, per_group = l.tiles ? kMfmaRowsPerItem : 16 * l.row_tiles * l.row_waves;
-    const auto tiles_of = [&](const FlpStepSeq& r) { return ((int64_t)r.prefix + r.n + tile - 1) / tile; };
-    const auto groups = [&](const FlpStepSeq& r) { return ((int64_t)r.n * G + per_group - 1) / per_group; };
-    std::stable_sort(l.recs.begin(), l.recs.end(), [&](const FlpStepSeq& x, const FlpStepSeq& y) { return tiles_of(x) > tiles_of(y); });
-    int64_t total = 0;
-    for (const FlpStepSeq& r : l.recs) total += groups(r) * tiles_of(r) * n_kv;
-    const int64_t piece = l.tiles ? std::max<int64_t>(kMinTilePiece, (total + kTileUnits - 1) / kTileUnits)
-                                  : std::max<int64_t>(kMinPiece * (4 / l.row_waves), (total + kUnits - 1) / kUnits);
-    for (FlpStepSeq& r : l.recs) {
-      r.pieces = (int32_t)std::min<int64_t>(kMaxPieces, (tiles_of(r) + piece - 1) / piece);
-      r.unit0 = (int32_t)l.units;
-      l.units += groups(r) * r.pieces;
-      r.part0 = (int32_t)parts;
-      r.merge0 = l.merge_rows;
-      if (r.pieces > 1) {
-        parts += (int64_t)r.n * r.pieces;
-        l.merge_rows += r.n;
+    std::stable_sort(l.recs.begin(), l.recs.end(), [&](const FlpStepSeq& x, const FlpStepSeq& y) { return length(x) > length(y); });
+    l.head_waves = l.row_waves = 1;
+    const int tile = l.tiles ? 64 : run;
+    if (!l.tiles) {
+      int64_t waves = 0, steps = 0;                    // were every row tile of every head one
+      for (const FlpStepSeq& r : l.recs) {
+        const int64_t x = over((int64_t)r.n * G, 16) * n_kv;
+        waves += x;
+        steps += x * over(length(r), tile);
+      }
+      if (waves >= 4 * kWaveSlots && rows > 16)
+        l.row_waves = 4;
+      else if (waves >= 4 * kWaveSlots && steps <= 16 * waves)
+        l.head_waves = 4;
+    }
+    const int per_group = l.tiles ? kMfmaRowsPerItem : 16 * l.row_waves;
+    tiles.clear();
+    groups.clear();
+    int64_t total = 0, units = 0;
+    for (const FlpStepSeq& r : l.recs) {
+      tiles.push_back(over(length(r), tile));
+      groups.push_back(over((int64_t)r.n * G, per_group));
+      units += groups.back() * n_kv;
+      total += groups.back() * tiles.back() * n_kv;
+    }
+    const int64_t longest = tiles[0];
+    int64_t piece = longest;
+    if (l.tiles) {
+      double best = 0;
+      for (int k = 1; k <= 16 && (k == 1 || over(longest, k) >= 4); ++k) {
+        const int64_t cand = over(longest, k);
+        int64_t n = 0, kept = 0;
+        double sum = 0;
+        for (size_t i = 0; i < tiles.size(); ++i) {
+          const int64_t pieces = over(tiles[i], cand);
+          const double us = 1.8 * tiles[i] / pieces + 4;
+          n += groups[i] * pieces * n_kv;
+          sum += us * groups[i] * pieces * n_kv;
+          if (pieces > 1) kept += pieces * l.recs[i].n;
+        }
+        const double idle = n % kTileSlots ? 1 - (double)(n % kTileSlots) / kTileSlots : 0;
+        const double us = sum / kTileSlots + idle * (sum / n) + (k > 1 ? 5 : 0) + kept * G * n_kv * 1040 / 4e6;
+        if (k == 1 || us < best) {
+          best = us;
+          piece = cand;
+        }
+      }
+      l.waves = 8;
+    } else {
+      l.waves = 4;
+      if (l.row_waves == 1 && l.head_waves == 1) {
+        if (units <= kWaveSlots / 2 && longest <= 28)
+          l.waves = 8;
+        else if (units <= kWaveSlots / 2)
+          piece = std::max<int64_t>(8, over(total, kWaveSlots));
+        else
+          piece = std::max<int64_t>(32, over(2 * total, kWaveSlots));
       }
     }
-    l.waves = l.row_tiles == 1 && l.units * n_kv <= 256 ? 8 : 4;
+    cut(l, piece, n_kv, tiles.data(), groups.data(), &parts);
     launches.push_back(std::move(l));
   }
   *part_rows = (size_t)parts;
@@ -249,20 +317,18 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
   const FlpStepSeq* at = slot ? (const FlpStepSeq*)slot->dev : nullptr;
   for (size_t i = 0; i < launches.size() && s == FLP_OK; ++i) {
     const AttnLaunch& l = launches[i];
-    FlpStepList list;
     a.n_recs = (int32_t)l.recs.size();
     a.merge_rows = l.merge_rows;
+    a.head_waves = l.head_waves;
     a.row_waves = l.row_waves;
     a.recs = nullptr;
-    if (inline_records(l.recs)) {
-      std::copy(l.recs.begin(), l.recs.end(), list.seq);
-    } else {
+    if (!inline_records(l.recs)) {
       a.recs = at;
       at += l.recs.size();
     }
-    s = l.tiles ? flp_launch_attn_step_tiles(p->cfg.dtype, a, list, l.units, stream)
-                : flp_launch_attn_step(p->cfg.dtype, p->cfg.head_dim, a, list, l.row_tiles, l.waves, l.units, stream);
-    if (s == FLP_OK) s = flp_launch_attn_step_merge(p->cfg.dtype, p->cfg.head_dim, a, list, stream);
+    s = l.tiles ? flp_launch_attn_step_tiles(p->cfg.dtype, a, l.recs.data(), l.units, stream)
+                : flp_launch_attn_step(p->cfg.dtype, p->cfg.head_dim, a, l.recs.data(), l.waves, l.units, stream);
+    if (s == FLP_OK) s = flp_launch_attn_step_merge(p->cfg.dtype, p->cfg.head_dim, a, l.recs.data(), stream);
   }
   if (!slot) return s;
   const flp_status released = flp_stage_release(slot, stream);
@@ -358,7 +424,7 @@ extern "C" flp_status flp_kv_accept(flp_pool* p, const flp_attn_batch* b, const 
     FLP_TRY(check_device(p, who));
     hipStream_t stream = (hipStream_t)hip_stream;
     const FlpStepArgs a = make_args(p, b, nullptr, kv8 == 1);
-    FlpSeqList list;
+    FlpSeqList<kListSeqs> list;
     for (int32_t first = 0; first < b->n_seqs; first += kListSeqs) {
       seq_list(b, first, &list);
       FLP_TRY(flp_launch_kv_accept(kv8 ? 1 : p->elem_bytes, p->cfg.head_dim, a, list, n_accept, path, stream));
