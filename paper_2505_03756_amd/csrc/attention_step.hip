@@ -105,9 +105,9 @@ __device__ __forceinline__ float got(float v, int) { return v; }
 __device__ __forceinline__ float got(h16x8 v, int e) { return (float)v[e]; }
 __device__ __forceinline__ float got(b16x8 v, int e) { return (float)v[e]; }
 
-// W waves per workgroup, NL records in the arguments
-template <typename S, int D, bool KV8, int W, int NL>
-__global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, FlpStepList<NL> list) {
+// W waves per workgroup; List: the records in the arguments
+template <typename S, int D, bool KV8, int W, typename List>
+__global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, List list) {
   typedef Kind<S, KV8> C;
   typedef typename C::kvec kvec;
   typedef typename C::vvec vvec;
@@ -117,6 +117,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Flp
   constexpr uint32_t ALL = (1u << RUN) - 1;
   __shared__ f32x4 merge_o[W][CT][64];
   __shared__ float2 merge_ml[W][16];
+  __shared__ uint8_t flags[W][CT][64];
 
   const int lane = threadIdx.x & 63, lr = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -125,7 +126,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Flp
   const int head_groups = (a.n_kv + hw - 1) / hw, u = blockIdx.x / head_groups;
   const int own_head = (blockIdx.x - u * head_groups) * hw + wave / per_head, in_head = wave % per_head;
   const int g = own_head < a.n_kv ? own_head : a.n_kv - 1;
-  const FlpStepSeq rec = flp_step_record(a, list, u, &FlpStepSeq::unit0);
+  const FlpStepSeq rec = flp_step_record(a, list, u);
   const int G = a.n_h / a.n_kv, R = rec.n * G, P = rec.prefix, L = P + rec.n;
   const int groups = (R + 16 * rw - 1) / (16 * rw);    // workgroups that the rows take
   const int local = u - rec.unit0, piece = local / groups, rgroup = local - piece * groups;
@@ -202,47 +203,50 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Flp
   for (int ct = 0; ct < CT; ++ct) O[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // V with values that are not finite: they are replaced by zero, and which sums they would have gone into is kept, a byte per four
-  // channels of a row, in the wave's part of the merge's LDS (bit e of vis: position e of the lane's run).  NaN counts as both infinities.
+  // channels of a row (bit e of vis: position e of the lane's run); NaN counts as both infinities.  By way of LDS, in a loop that is not
+  // unrolled: what is hardly ever run should cost neither registers nor code.
   bool flagged = false;
-  uint8_t* const flags = reinterpret_cast<uint8_t*>(&merge_o[wave][0][0]) + lane;
   const auto not_finite = [&](uint32_t vis) __attribute__((always_inline)) {
-    if (!flagged)
-#pragma unroll 1
-      for (int x = 0; x < CT; ++x) flags[64 * x] = 0;
-    flagged = true;
+    u32x4* const hold = reinterpret_cast<u32x4*>(&merge_o[wave][0][0]) + lane;
+    uint8_t* const flag = &flags[wave][0][lane];
 #pragma unroll
+    for (int ct = 0; ct < CT; ++ct) hold[64 * ct] = vr[ct];
+#pragma unroll 1
     for (int ct = 0; ct < CT; ++ct) {
-      uint32_t f = 0;
+      u32x4 v = hold[64 * ct];
+      uint32_t f = flagged ? flag[64 * ct] : 0u;
 #pragma unroll
       for (int sign = 0; sign < (KV8 ? 1 : 2); ++sign) {             // e4m3 has no infinities
         f32x4 n = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-          const vvec x = C::v(vr[ct], s);
-          uint32_t b = vis;
-          asm volatile("" : "+v"(b));                  // here each time: kept for all channels the indicators would cost registers
+          const vvec x = C::v(v, s);
           vvec is, seen;
 #pragma unroll
           for (int e = 0; e < VE; ++e) {
             const float y = got(x, e);
             put(is, e, y != y || y == (sign ? -INFINITY : INFINITY) ? 1.f : 0.f);
-            put(seen, e, (b >> (VE * s + e)) & 1 ? 1.f : 0.f);
+            put(seen, e, (vis >> (VE * s + e)) & 1 ? 1.f : 0.f);
           }
           n = mma(is, seen, n);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) f |= n[i] > 0.f ? (KV8 ? 0x11u : sign ? 0x10u : 1u) << i : 0u;
       }
-      flags[64 * ct] |= (uint8_t)f;
+      flag[64 * ct] = (uint8_t)f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {                    // the high bit of each such value, spread over it
-        const uint32_t o = C::odd(vr[ct][w]);
-        vr[ct][w] &= ~(C::ES == 4 ? 0u - (o >> 31) : C::ES == 2 ? (o >> 15) * 0xffffu : (o >> 7) * 0xffu);
+        const uint32_t o = C::odd(v[w]);
+        v[w] &= ~(C::ES == 4 ? 0u - (o >> 31) : C::ES == 2 ? (o >> 15) * 0xffffu : (o >> 7) * 0xffu);
       }
-      __builtin_amdgcn_sched_barrier(0);
+      hold[64 * ct] = v;
     }
+    flagged = true;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) vr[ct] = hold[64 * ct];
   };
 
+  // one tile; the registers of K and V are filled with the wave's next tile as soon as they are used up
   const auto step = [&](int tile) __attribute__((always_inline)) {
     const int next = tile + kw;
     const bool more = next < hi;
@@ -360,16 +364,6 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Flp
 
   if (works)
     for (int tile = tile0; tile < hi; tile += kw) step(tile);
-  if (flagged)
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      const uint32_t f = flags[64 * ct];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if ((f >> i) & 1) O[ct][i] += INFINITY;
-        if ((f >> (4 + i)) & 1) O[ct][i] -= INFINITY;
-      }
-    }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
 
@@ -379,6 +373,18 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Flp
   if (lh == 0) merge_ml[wave][lr] = make_float2(m, l);
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) merge_o[wave][ct][lane] = O[ct];
+  if (__builtin_expect(flagged, 0))
+#pragma unroll 1
+    for (int ct = 0; ct < CT; ++ct) {
+      const uint32_t f = flags[wave][ct][lane];
+      f32x4 o = merge_o[wave][ct][lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if ((f >> i) & 1) o[i] += INFINITY;
+        if ((f >> (4 + i)) & 1) o[i] -= INFINITY;
+      }
+      merge_o[wave][ct][lane] = o;
+    }
   __syncthreads();
   if (!active) return;
   const int first = wave - slice * rw;
@@ -426,8 +432,8 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Flp
 }
 
 // The pieces of a (token, head) row, at most 64, in piece order: a wave per row, lane i piece i's maximum and sum, every lane its channels
-template <typename S, int D, int NL>
-__global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, FlpStepList<NL> list) {
+template <typename S, int D, typename List>
+__global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, List list) {
   typedef typename S::storage ST;
   constexpr int CPL = D / 64;
   typedef float chan __attribute__((ext_vector_type(CPL)));
@@ -435,7 +441,7 @@ __global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, Flp
   const int64_t wid = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = (int)(wid / a.n_h), h = (int)(wid - (int64_t)row * a.n_h);
   if (row >= a.merge_rows) return;
-  const FlpStepSeq rec = flp_step_record(a, list, row, &FlpStepSeq::merge0);
+  const FlpStepSeq rec = flp_step_record<true>(a, list, row);
   const int tok = row - rec.merge0, ns = rec.pieces;
   const int64_t stride = (int64_t)a.n_h * (D + 2);
   const float* __restrict__ pp = a.partials + ((int64_t)rec.part0 + (int64_t)tok * ns) * stride + (int64_t)h * (D + 2);
@@ -479,12 +485,12 @@ __global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, Flp
 template <typename S, int D>
 void launch_kind(const FlpStepArgs& a, const FlpStepSeq* recs, int waves, unsigned grid, hipStream_t stream) {
   flp_with_records(a, recs, [&](const auto& list) {
-    constexpr int NL = sizeof(list.seq) / sizeof(FlpStepSeq);
+    typedef typename std::decay<decltype(list)>::type L;
     const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), 0, stream, a, list); };
     if constexpr (!std::is_same<S, F32>::value)
       if (a.k_scale)
-        return waves == 8 ? launch(attn_step_kernel<S, D, true, 8, NL>) : launch(attn_step_kernel<S, D, true, 4, NL>);
-    waves == 8 ? launch(attn_step_kernel<S, D, false, 8, NL>) : launch(attn_step_kernel<S, D, false, 4, NL>);
+        return waves == 8 ? launch(attn_step_kernel<S, D, true, 8, L>) : launch(attn_step_kernel<S, D, true, 4, L>);
+    waves == 8 ? launch(attn_step_kernel<S, D, false, 8, L>) : launch(attn_step_kernel<S, D, false, 4, L>);
   });
 }
 
@@ -511,15 +517,15 @@ flp_status flp_launch_attn_step_merge(int dtype, int head_dim, const FlpStepArgs
   if (a.merge_rows <= 0) return FLP_OK;
   const dim3 grid((unsigned)(((int64_t)a.merge_rows * a.n_h + 3) / 4));
   flp_with_records(a, inline_recs, [&](const auto& list) {
-    constexpr int NL = sizeof(list.seq) / sizeof(FlpStepSeq);
+    typedef typename std::decay<decltype(list)>::type L;
     const bool d64 = head_dim == 64;
     const auto merge = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, list); };
     if (dtype == FLP_F32)
-      d64 ? merge(attn_step_merge_kernel<F32, 64, NL>) : merge(attn_step_merge_kernel<F32, 128, NL>);
+      d64 ? merge(attn_step_merge_kernel<F32, 64, L>) : merge(attn_step_merge_kernel<F32, 128, L>);
     else if (dtype == FLP_F16)
-      d64 ? merge(attn_step_merge_kernel<F16, 64, NL>) : merge(attn_step_merge_kernel<F16, 128, NL>);
+      d64 ? merge(attn_step_merge_kernel<F16, 64, L>) : merge(attn_step_merge_kernel<F16, 128, L>);
     else
-      d64 ? merge(attn_step_merge_kernel<BF16, 64, NL>) : merge(attn_step_merge_kernel<BF16, 128, NL>);
+      d64 ? merge(attn_step_merge_kernel<BF16, 64, L>) : merge(attn_step_merge_kernel<BF16, 128, L>);
   });
   FLP_TRY_HIP(hipGetLastError());
   return FLP_OK;

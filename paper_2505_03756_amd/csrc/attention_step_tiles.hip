@@ -46,8 +46,8 @@ __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi) {
   return w;
 }
 
-template <typename M, bool KV8, int NL>
-__global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, FlpStepList<NL> list) {
+template <typename M, bool KV8, typename List>
+__global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, List list) {
   typedef typename M::vec vec;                                       // scores
   typedef typename std::conditional<KV8, MF16, M>::type MV;          // second product
   typedef typename MV::vec wvec;
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int u = blockIdx.x / a.n_kv, g = blockIdx.x - u * a.n_kv;
-  const FlpStepSeq rec = flp_step_record(a, list, u, &FlpStepSeq::unit0);
+  const FlpStepSeq rec = flp_step_record(a, list, u);
   const int G = a.n_h / a.n_kv, R = rec.n * G, P = rec.prefix, L = P + rec.n;
   const int groups = (R + kMfmaRowsPerItem - 1) / kMfmaRowsPerItem;
   const int local = u - rec.unit0, piece = local / groups;
@@ -448,14 +448,14 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
 flp_status flp_launch_attn_step_tiles(int dtype, const FlpStepArgs& a, const FlpStepSeq* inline_recs, int64_t n_units, hipStream_t stream) {
   if (n_units <= 0) return FLP_OK;
   flp_with_records(a, inline_recs, [&](const auto& list) {
-    constexpr int NL = sizeof(list.seq) / sizeof(FlpStepSeq);
+    typedef typename std::decay<decltype(list)>::type L;
     const auto launch = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)(n_units * a.n_kv)), dim3(512), 0, stream, a, list);
     };
     if (dtype == FLP_F16)
-      a.k_scale ? launch(attn_step_tiles_kernel<MF16, true, NL>) : launch(attn_step_tiles_kernel<MF16, false, NL>);
+      a.k_scale ? launch(attn_step_tiles_kernel<MF16, true, L>) : launch(attn_step_tiles_kernel<MF16, false, L>);
     else
-      a.k_scale ? launch(attn_step_tiles_kernel<MBF16, true, NL>) : launch(attn_step_tiles_kernel<MBF16, false, NL>);
+      a.k_scale ? launch(attn_step_tiles_kernel<MBF16, true, L>) : launch(attn_step_tiles_kernel<MBF16, false, L>);
   });
   FLP_TRY_HIP(hipGetLastError());
   return FLP_OK;

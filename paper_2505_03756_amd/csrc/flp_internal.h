@@ -207,7 +207,8 @@ struct FlpSeqList {
   int32_t t0[N + 1], prefix[N], unit0[N];
 };
 // The attention launches have one record per sequence with new tokens: `unit0` is the first of the launch's workgroup units that
-// belong to it.  Up to kStepInline records travel in the launch's own arguments, more of them through a staging slot.
+// belong to it.  They travel in the launch's own arguments as far as those hold them: kStepInline of them, kStepPacked where no context is
+// cut into pieces and the numbers fit 16 bits; more of them through a staging slot.
 struct FlpStepSeq {
   int32_t seq;                 // row of the block tables
   int32_t t0, n, prefix;       // first new token, new tokens, positions before them
@@ -219,6 +220,13 @@ template <int N>
 struct FlpStepList {
   FlpStepSeq seq[N];
 };
+constexpr int kStepPacked = 224;
+struct FlpStepPacked {
+  struct {
+    uint32_t seq_n;            // seq | n << 16
+    int32_t t0, prefix, unit0;
+  } seq[kStepPacked];
+};
 struct FlpStepArgs {
   uint8_t* pool;
   int64_t block_bytes;
@@ -227,6 +235,7 @@ struct FlpStepArgs {
   int32_t n_h, n_kv;
   int32_t pb;                  // positions per block of this cache: 16, 32 or 64
   int32_t n_recs, merge_rows;
+  int32_t units_each;          // units of every record, 0 where they differ
   int32_t head_waves, row_waves;   // attention: waves of a workgroup side by side on kv heads and on row tiles (1, or one of them 4)
   float scale_log2e;
   const FlpStepSeq* recs;      // null: in the launch's arguments

@@ -115,7 +115,6 @@ FlpStepArgs make_args(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_
   return a;
 }
 
-bool inline_records(const std::vector<FlpStepSeq>& recs) { return recs.size() <= (size_t)kStepInline; }
 
 // Staging slots and the workspace are handed from call to call by events, which a replayed graph would not see
 flp_status refuse_capture(hipStream_t stream, const char* who) {
@@ -160,20 +159,28 @@ struct AttnLaunch {
   std::vector<FlpStepSeq> recs;
   bool tiles;                  // attention_step_tiles.hip
   int32_t head_waves, row_waves, waves, merge_rows;
-  int64_t units;
+  int64_t units, units_each;   // units_each: of every record, 0 where they differ
 };
+
+bool inline_records(const AttnLaunch& l) {
+  if (l.merge_rows || l.recs.size() <= (size_t)kShortList) return l.recs.size() <= (size_t)kStepInline;
+  return l.recs.size() <= (size_t)kStepPacked &&
+         std::all_of(l.recs.begin(), l.recs.end(), [](const FlpStepSeq& r) { return r.seq < 65536 && r.n < 65536; });
+}
 
 constexpr int kMaxPieces = 64;
 constexpr int kWaveSlots = 512, kTileSlots = 256;      // workgroups of four waves, and of the tiled kernel, that the chip holds at once
 
 void cut(AttnLaunch& l, int64_t piece, int n_kv, const int64_t* tiles, const int64_t* groups, int64_t* parts) {
-  l.units = 0;
+  l.units = l.units_each = 0;
   l.merge_rows = 0;
   for (size_t i = 0; i < l.recs.size(); ++i) {
     FlpStepSeq& r = l.recs[i];
     r.pieces = (int32_t)std::min<int64_t>(kMaxPieces, (tiles[i] + piece - 1) / piece);
     r.unit0 = (int32_t)l.units;
-    l.units += groups[i] * r.pieces;
+    const int64_t units = groups[i] * r.pieces;
+    l.units_each = i == 0 || l.units_each == units ? units : 0;
+    l.units += units;
     r.part0 = (int32_t)*parts;
     r.merge0 = l.merge_rows;
     if (r.pieces > 1) {
@@ -227,9 +234,10 @@ std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, cons
         waves += x;
         steps += x * over(length(r), tile);
       }
-      if (waves >= 4 * kWaveSlots && rows > 16)
+      const bool few_steps = waves >= 768 && steps <= 4 * waves;
+      if (rows > 32 && (waves >= 4 * kWaveSlots || few_steps))
         l.row_waves = 4;
-      else if (waves >= 4 * kWaveSlots && steps <= 16 * waves)
+      else if (few_steps || (waves >= 4 * kWaveSlots && steps <= 16 * waves))
         l.head_waves = 4;
     }
     const int per_group = l.tiles ? kMfmaRowsPerItem : 16 * l.row_waves;
@@ -295,7 +303,7 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
       flp_set_error("%s: more rows than one launch takes", who);
       return FLP_ERANGE;
     }
-    staged += inline_records(l.recs) ? 0 : l.recs.size();
+    staged += inline_records(l) ? 0 : l.recs.size();
   }
   FlpStageSlot* slot = nullptr;
   FlpStepArgs a = make_args(p, b, sc, sc != nullptr);
@@ -310,7 +318,7 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
     FLP_TRY(flp_stage_acquire(p, staged * sizeof(FlpStepSeq), &slot));
     FlpStepSeq* to = (FlpStepSeq*)slot->host;
     for (const AttnLaunch& l : launches)
-      if (!inline_records(l.recs)) to = std::copy(l.recs.begin(), l.recs.end(), to);
+      if (!inline_records(l)) to = std::copy(l.recs.begin(), l.recs.end(), to);
   }
   flp_status s = staged ? flp_stage_upload(slot, staged * sizeof(FlpStepSeq), stream) : FLP_OK;
   if (s == FLP_OK && with_append8) s = append8(p, b, sc, stream);
@@ -319,10 +327,11 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
     const AttnLaunch& l = launches[i];
     a.n_recs = (int32_t)l.recs.size();
     a.merge_rows = l.merge_rows;
+    a.units_each = (int32_t)l.units_each;
     a.head_waves = l.head_waves;
     a.row_waves = l.row_waves;
     a.recs = nullptr;
-    if (!inline_records(l.recs)) {
+    if (!inline_records(l)) {
       a.recs = at;
       at += l.recs.size();
     }
