@@ -127,7 +127,8 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
   const int sblk = wave >> 1;
   const int64_t k_region = (int64_t)g * pb * D * ES, v_region = (int64_t)(a.n_kv + g) * pb * D * ES;
   uint32_t kg[2], vg[2], lds_wave = 0;
-  // 8 bit: a thread's 16 channels of key 8 w + lane / 8, and 16 positions of channel 32 (w % 4) + lane / 2
+  // 8 bit: a thread's 16 channels of key 8 w + lane / 8, and 16 positions of channel 32 (w % 4) + lane % 32 (so that what 16 lanes
+  // write to LDS lies in different banks)
   u32x4 rawk, rawv;
   int32_t next_k = 0, next_v = 0;                                    // blocks of the tile that is requested next
   if constexpr (!KV8) {
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
     }
     lds_wave = (uint32_t)(uintptr_t)(lds_u8*)smem + sblk * 4096 + 2 * (wave & 1) * 1024;
   }
-  const int vch = 32 * (wave & 3) + (lane >> 1), vgrp = 2 * (wave >> 2) + (lane & 1);
+  const int vch = 32 * (wave & 3) + (lane & 31), vgrp = 2 * (wave >> 2) + (lane >> 5);
   __builtin_amdgcn_s_waitcnt(kWaitVm0);                              // from here on only tile loads are in flight
   __syncthreads();
 
