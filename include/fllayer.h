@@ -118,6 +118,21 @@ flp_status fll_layer_forward(flp_pool* pool, const fll_layer_config* cfg, const 
                              const fll_layer_batch* batch, void* h, void* scratch, int64_t scratch_bytes,
                              void* hip_stream);
 
+/* What a layer may do otherwise; a NULL pointer leaves the layer as it is. */
+typedef struct {
+  const void*     q_norm;     /* [head_dim], pool type: norms of queries and keys per head (fll_qk_norm_rope, with the  */
+  const void*     k_norm;     /*   layer's eps) in the place of fll_rope; both or neither                               */
+  const uint64_t* tree_mask;  /* device uint64[n_tokens]: the new tokens are trees (flp_paged_tree_attention; `positions`
+                                 then holds prefix_len[i] + a token's depth in its tree)                               */
+  const float*    k_scale;    /* device float[n_kv_heads]: the sequences' cache is in 8 bits (flp_kv_append8 and its    */
+  const float*    v_scale;    /*   attention); both or neither                                                          */
+} fll_layer_options;
+
+/* fll_layer_forward with options (NULL: none). */
+flp_status fll_layer_forward_options(flp_pool* pool, const fll_layer_config* cfg, const fll_layer_weights* w,
+                                     const fll_layer_batch* batch, const fll_layer_options* options, void* h, void* scratch,
+                                     int64_t scratch_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

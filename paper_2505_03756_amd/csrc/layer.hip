@@ -604,13 +604,43 @@ extern "C" int64_t fll_layer_scratch_bytes(const flp_pool* pool, const fll_layer
   return (int64_t)layout(pool, cfg, n_tokens).total;
 }
 
+namespace {
+// what of a layer's options the host can see to be wrong, before anything is enqueued
+flp_status check_options(const flp_pool* p, const fll_layer_batch* b, const fll_layer_options& o) {
+  if (!o.q_norm != !o.k_norm || !o.k_scale != !o.v_scale || !aligned16(o.q_norm) || !aligned16(o.k_norm) ||
+      (((uintptr_t)o.k_scale | (uintptr_t)o.v_scale) & 3) || ((uintptr_t)o.tree_mask & 7)) {
+    flp_set_error("fll_layer_forward_options: one of a pair of pointers is null, or one is misaligned");
+    return FLP_EINVAL;
+  }
+  if (o.k_scale && p->elem_bytes == 4) {
+    flp_set_error("fll_layer_forward_options: an fp32 pool holds no 8-bit cache");
+    return FLP_ENOTSUP;
+  }
+  if (o.tree_mask && b->cu_new)
+    for (int32_t i = 0; i < b->n_seqs; ++i)
+      if ((int64_t)b->cu_new[i + 1] - b->cu_new[i] > 64) {
+        flp_set_error("fll_layer_forward_options: sequence %d has more than the 64 new tokens of a tree", i);
+        return FLP_ERANGE;
+      }
+  return FLP_OK;
+}
+}  // namespace
+
 extern "C" flp_status fll_layer_forward(flp_pool* p, const fll_layer_config* c, const fll_layer_weights* w,
                                         const fll_layer_batch* b, void* h, void* scratch, int64_t scratch_bytes,
                                         void* hip_stream) {
+  return fll_layer_forward_options(p, c, w, b, nullptr, h, scratch, scratch_bytes, hip_stream);
+}
+
+extern "C" flp_status fll_layer_forward_options(flp_pool* p, const fll_layer_config* c, const fll_layer_weights* w,
+                                                const fll_layer_batch* b, const fll_layer_options* options, void* h, void* scratch,
+                                                int64_t scratch_bytes, void* hip_stream) {
   if (!cfg_ok(p, c) || !w || !b || !h || !scratch || b->n_tokens < 0 || b->n_seqs < 0) {
     flp_set_error("fll_layer_forward: null argument or bad layer shape");
     return FLP_EINVAL;
   }
+  const fll_layer_options opt = options ? *options : fll_layer_options{};
+  FLP_TRY(check_options(p, b, opt));
   if (!w->in_norm || !w->post_norm || !w->wq || !w->wk || !w->wv || !w->wo || !w->w_gate || !w->w_up || !w->w_down) {
     flp_set_error("fll_layer_forward: a weight pointer is null");
     return FLP_EINVAL;
@@ -709,7 +739,11 @@ extern "C" flp_status fll_layer_forward(flp_pool* p, const fll_layer_config* c, 
     const void* const ws[3] = {w->wq, w->wk, w->wv};
     FLP_TRY(project(n, H, 3, which, ys, d_outs, ws));
   }
-  FLP_TRY(fll_rope(dtype, q, k, b->positions, T, c->n_q_heads, n_kv, d, theta, hip_stream));
+  if (opt.q_norm)
+    FLP_TRY(fll_qk_norm_rope(dtype, q, Hq, k, Hkv, opt.q_norm, opt.k_norm, b->positions, q, k, T, c->n_q_heads, n_kv, d, eps, theta,
+                             hip_stream));
+  else
+    FLP_TRY(fll_rope(dtype, q, k, b->positions, T, c->n_q_heads, n_kv, d, theta, hip_stream));
   {
     flp_attn_batch ab{};
     ab.n_seqs = b->n_seqs;
@@ -723,7 +757,13 @@ extern "C" flp_status fll_layer_forward(flp_pool* p, const fll_layer_config* c, 
     ab.cu_new = b->cu_new;
     ab.prefix_len = b->prefix_len;
     ab.block_tables = b->kv_tables;
-    FLP_TRY(flp_paged_prefix_attention(p, &ab, hip_stream));
+    const flp_kv8_scales scales{opt.k_scale, opt.v_scale};
+    if (opt.tree_mask)
+      FLP_TRY(flp_paged_tree_attention(p, &ab, opt.tree_mask, opt.k_scale ? &scales : nullptr, hip_stream));
+    else if (opt.k_scale)
+      FLP_TRY(flp_paged_prefix_attention8(p, &ab, &scales, hip_stream));
+    else
+      FLP_TRY(flp_paged_prefix_attention(p, &ab, hip_stream));
   }
   {
     const int which[1] = {3}, d_outs[1] = {H};

@@ -10,7 +10,7 @@ from . import flpool
 from .flpool import _check, _ptr, _stream
 
 EXPORTS = ("fll_rmsnorm", "fll_add_rmsnorm", "fll_rope", "fll_qk_norm_rope", "fll_silu_mul", "fll_layer_scratch_bytes",
-           "fll_layer_forward")
+           "fll_layer_forward", "fll_layer_forward_options")
 PROJ_ORDER = ("q", "k", "v", "o", "gate", "up", "down")
 
 
@@ -35,6 +35,10 @@ class LayerBatch(C.Structure):
                 ("lora", LoraPlace * 7)]
 
 
+class LayerOptions(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_norm", "k_norm", "tree_mask", "k_scale", "v_scale")]
+
+
 _ready = False
 
 
@@ -54,6 +58,8 @@ def _lib():
         L.fll_layer_scratch_bytes.restype = i64
         L.fll_layer_forward.argtypes = [vp, C.POINTER(LayerConfig), C.POINTER(LayerWeights), C.POINTER(LayerBatch), vp,
                                         vp, i64, vp]
+        L.fll_layer_forward_options.argtypes = [vp, C.POINTER(LayerConfig), C.POINTER(LayerWeights), C.POINTER(LayerBatch),
+                                                C.POINTER(LayerOptions), vp, vp, i64, vp]
         _ready = True
     return L
 
@@ -106,7 +112,15 @@ class Layer:
             raise flpool.FlpError(flpool.FLP_EINVAL, "fll_layer_scratch_bytes: bad layer shape")
         return int(n)
 
-    def forward(self, batch, h, scratch, scratch_bytes, stream=None):
+    def forward(self, batch, h, scratch, scratch_bytes, stream=None, q_norm=None, k_norm=None, tree_mask=None, k_scale=None,
+                v_scale=None):
+        """q_norm, k_norm: norms of queries and keys per head; tree_mask: the new tokens are trees; k_scale, v_scale: the cache is
+        in 8 bits (device tensors, see fll_layer_options)."""
+        if not all(x is None for x in (q_norm, k_norm, tree_mask, k_scale, v_scale)):
+            opt = LayerOptions(_ptr(q_norm), _ptr(k_norm), _ptr(tree_mask), _ptr(k_scale), _ptr(v_scale))
+            _check(_lib().fll_layer_forward_options(self.pool._h, C.byref(self.cfg), C.byref(self.w), C.byref(batch.c),
+                                                    C.byref(opt), _ptr(h), _ptr(scratch), scratch_bytes, _stream(stream)))
+            return
         _check(_lib().fll_layer_forward(self.pool._h, C.byref(self.cfg), C.byref(self.w), C.byref(batch.c), _ptr(h),
                                         _ptr(scratch), scratch_bytes, _stream(stream)))
 
