@@ -19,10 +19,11 @@ __device__ __forceinline__ float quotient(float x, float s, float r) {
   return x != x ? x : copysignf(q, x);
 }
 
-// Workgroups of K and workgroups of V per unit of 32 slots and 1024 elements of a token's row; all reads of a thread are on their
-// way together.  K: a thread owns 8 channels of 16 slots.  V: a thread owns 4 channels and turns their 32 slots into their 32-byte runs of
-// the transposed V, whole sectors.  A unit that covers part of its run (the ends of a sequence's new tokens) merges its slots into the
-// 16-byte words already there, which belong to this sequence alone; units of one or two slots (a decode batch) store single bytes.
+// Workgroups of K and workgroups of V per unit of 32 slots and 1024 elements of a token's row; a thread owns 8 channels of 16 slots, and all
+// its reads are on their way together.  V is turned in registers into the channels' 16-byte half runs of the transposed layout; the two
+// halves of a run come from one workgroup.  A unit that covers part of its run (the ends of a sequence's new tokens) merges its
+// slots into the words already there, which belong to this sequence alone; units of one or two slots (a decode batch) store
+// single bytes, and are bound by these: 32 bytes apart, a sector each.
 template <typename S, int D, int N>
 __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqList<N> list) {
   typedef typename S::storage ST;
@@ -45,90 +46,73 @@ __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqLi
   const int slot0 = run * SL & (a.pb - 1);
   const int64_t blk = a.tables[(int64_t)(list.seq0 + rec) * a.max_blocks + run * SL / a.pb];
   uint8_t* const base = a.pool + blk * a.block_bytes;
-  const auto bytes4 = [](const ST* e, float s, float r) {
-    float f[4];
+  const int e0 = (blockIdx.y >> 1) * 1024 + (threadIdx.x & 127) * 8, h = threadIdx.x >> 7;
+  if (e0 >= row || s1 <= 16 * h || s0 >= 16 * h + 16) return;
+  const int g = e0 / D;
+  const float scale = is_v ? a.v_scale[g] : a.k_scale[g], r = 1.f / scale;
+  const ST* const src = reinterpret_cast<const ST*>(is_v ? a.v_new : a.k_new) + t0 * row + e0;
+  uint8_t* const dst = base + (is_v ? (int64_t)row * a.pb + (int64_t)e0 * a.pb + slot0 : ((int64_t)g * a.pb + slot0) * D + (e0 - g * D));
+  const auto bytes8 = [&](u32x4 x) {
+    ST e[8];
+    __builtin_memcpy(e, &x, 16);
+    float f[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = quotient(S::to_float(e[i]), s, r);
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], w, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
+    for (int i = 0; i < 8; ++i) f[i] = quotient(S::to_float(e[i]), scale, r);
+    uint2 w = make_uint2(0, 0);
+    w.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], w.x, false);
+    w.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w.x, true);
+    w.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[4], f[5], w.y, false);
+    w.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[6], f[7], w.y, true);
     return w;
   };
-  if (!is_v) {
-    const int e0 = (blockIdx.y >> 1) * 1024 + (threadIdx.x & 127) * 8, h = threadIdx.x >> 7;
-    if (e0 >= row) return;
-    const int g = e0 / D;
-    const float scale = a.k_scale[g], r = 1.f / scale;
-    uint8_t* const dst = base + ((int64_t)g * a.pb + slot0) * D + (e0 - g * D);
-    const ST* const src = reinterpret_cast<const ST*>(a.k_new) + t0 * row + e0;
-    u32x4 x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int s = 16 * h + i;
-      if (s >= s0 && s < s1) x[i] = *reinterpret_cast<const u32x4*>(src + (int64_t)s * row);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int s = 16 * h + i;
-      if (s < s0 || s >= s1) continue;
-      ST e[8];
-      __builtin_memcpy(e, &x[i], 16);
-      *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = make_uint2(bytes4(e, scale, r), bytes4(e + 4, scale, r));
-    }
-    return;
-  }
-  const int e0 = (blockIdx.y >> 1) * 1024 + threadIdx.x * 4;
-  if (e0 >= row) return;
-  const float scale = a.v_scale[e0 / D], r = 1.f / scale;
-  uint8_t* const dst = base + (int64_t)row * a.pb + (int64_t)e0 * a.pb + slot0;
-  const ST* const src = reinterpret_cast<const ST*>(a.v_new) + t0 * row + e0;
-  const auto fetch = [&](int s) { return *reinterpret_cast<const uint2*>(src + (int64_t)s * row); };
-  const auto word = [&](uint2 x) {
-    ST e[4];
-    __builtin_memcpy(e, &x, 8);
-    return bytes4(e, scale, r);
-  };
   if (s1 - s0 <= 2) {
-    for (int s = s0; s < s1; ++s) {
-      const uint32_t w = word(fetch(s));
+    for (int s = s0 > 16 * h ? s0 : 16 * h; s < s1 && s < 16 * h + 16; ++s) {
+      const uint2 w = bytes8(*reinterpret_cast<const u32x4*>(src + (int64_t)s * row));
+      if (!is_v) {
+        *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = w;
+        continue;
+      }
 #pragma unroll
-      for (int c = 0; c < 4; ++c) dst[(int64_t)c * a.pb + s] = (uint8_t)(w >> (8 * c));
+      for (int c = 0; c < 8; ++c) dst[(int64_t)c * a.pb + s] = (uint8_t)((c < 4 ? w.x : w.y) >> (8 * (c & 3)));
     }
     return;
   }
-  uint2 x[SL];
+  u32x4 x[16];
 #pragma unroll
-  for (int s = 0; s < SL; ++s)
-    if (s >= s0 && s < s1) x[s] = fetch(s);
+  for (int i = 0; i < 16; ++i) {
+    const int s = 16 * h + i;
+    if (s >= s0 && s < s1) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (int64_t)s * row));
+  }
+  uint2 by_slot[16];
 #pragma unroll
-  for (int h = 0; h < SL / 16; ++h) {
-    if (s1 <= 16 * h || s0 >= 16 * h + 16) continue;
-    uint32_t by_slot[16];
+  for (int i = 0; i < 16; ++i) {
+    const int s = 16 * h + i;
+    by_slot[i] = bytes8(x[i]);
+    if (!is_v && s >= s0 && s < s1) *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = by_slot[i];
+  }
+  if (!is_v) return;
 #pragma unroll
-    for (int s = 0; s < 16; ++s) by_slot[s] = word(x[16 * h + s]);
+  for (int c = 0; c < 8; ++c) {
+    u32x4* const at = reinterpret_cast<u32x4*>(dst + (int64_t)c * a.pb + 16 * h);
+    u32x4 w;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      u32x4* const at = reinterpret_cast<u32x4*>(dst + (int64_t)c * a.pb + 16 * h);
-      u32x4 w;
+    for (int q = 0; q < 4; ++q) {
+      uint32_t b = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b |= (((c < 4 ? by_slot[4 * q + i].x : by_slot[4 * q + i].y) >> (8 * (c & 3))) & 0xffu) << (8 * i);
+      w[q] = b;
+    }
+    if (s0 > 16 * h || s1 < 16 * h + 16) {
+      const u32x4 old = *at;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        uint32_t b = 0;
+        uint32_t mask = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) b |= ((by_slot[4 * q + i] >> (8 * c)) & 0xffu) << (8 * i);
-        w[q] = b;
+        for (int i = 0; i < 4; ++i) mask |= 16 * h + 4 * q + i >= s0 && 16 * h + 4 * q + i < s1 ? 0xffu << (8 * i) : 0u;
+        w[q] = (w[q] & mask) | (old[q] & ~mask);
       }
-      if (s0 > 16 * h || s1 < 16 * h + 16) {
-        const u32x4 old = *at;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t mask = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mask |= 16 * h + 4 * q + i >= s0 && 16 * h + 4 * q + i < s1 ? 0xffu << (8 * i) : 0u;
-          w[q] = (w[q] & mask) | (old[q] & ~mask);
-        }
-      }
-      *at = w;
     }
+    *at = w;
   }
 }
 

@@ -36,6 +36,21 @@ __device__ __forceinline__ void stv(void* p, const Vec<S>& v) {
   *reinterpret_cast<u32x4*>(p) = raw;
 }
 
+// past the caches' reuse: streams that the caches cannot hold until somebody reads them again
+template <typename S>
+__device__ __forceinline__ Vec<S> ldv_stream(const void* p) {
+  Vec<S> v;
+  const u32x4 raw = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  __builtin_memcpy(&v, &raw, 16);
+  return v;
+}
+template <typename S>
+__device__ __forceinline__ void stv_stream(void* p, const Vec<S>& v) {
+  u32x4 raw;
+  __builtin_memcpy(&raw, &v, 16);
+  __builtin_nontemporal_store(raw, reinterpret_cast<u32x4*>(p));
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -196,6 +211,10 @@ __global__ __launch_bounds__(256) void rope_kernel(typename S::storage* __restri
 // between neighbours and a value is rounded once, when it is stored.  One wave takes U x HPW heads of one token; all loads are under way
 // while it computes the token's angles, one per lane: turns in fp64 (position times theta^(-2i/d) / 2 pi, of which only the
 // fraction matters), sine and cosine of the fraction in fp32, shared through the wave's part of LDS.
+//
+// Bound by latency for a few tokens (8 of 64 + 8 heads: 3.4 us) and by memory for many.  U is 4 and accesses are non-temporal where the
+// tensors exceed the L2 caches: 8897 tokens of 40 + 40 heads, fp16, 364 MB: 80 us with U = 1, 77.6 with 4, 76.0 with U = 1 and
+// non-temporal accesses, 69.1 with both (5.3 TB/s; a copy reaches 4.9 to 5.6).
 struct TurnTable {
   double per_position[64];     // theta^(-2 i / d) / (2 pi)
 };
@@ -226,8 +245,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRows a, TurnTable t
     if (h >= heads) break;
     const ST* p = h < a.n_q ? (const ST*)a.q_in + (int64_t)t * a.ld_q_in + (int64_t)h * D
                             : (const ST*)a.k_in + (int64_t)t * a.ld_k_in + (int64_t)(h - a.n_q) * D;
-    x[u][0] = ldv<S>(p + c0);
-    x[u][1] = ldv<S>(p + HALF + c0);
+    x[u][0] = U > 1 ? ldv_stream<S>(p + c0) : ldv<S>(p + c0);
+    x[u][1] = U > 1 ? ldv_stream<S>(p + HALF + c0) : ldv<S>(p + HALF + c0);
   }
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
@@ -273,8 +292,13 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRows a, TurnTable t
       ob.e[j] = S::from_float(bf * cv[j] + af * sv[j]);
     }
     ST* o = is_q ? (ST*)a.q_out + ((int64_t)t * a.n_q + h) * D : (ST*)a.k_out + ((int64_t)t * a.n_kv + (h - a.n_q)) * D;
-    stv<S>(o + c0, oa);
-    stv<S>(o + HALF + c0, ob);
+    if (U > 1) {
+      stv_stream<S>(o + c0, oa);
+      stv_stream<S>(o + HALF + c0, ob);
+    } else {
+      stv<S>(o + c0, oa);
+      stv<S>(o + HALF + c0, ob);
+    }
   }
 }
 
@@ -445,7 +469,8 @@ extern "C" flp_status fll_qk_norm_rope(int32_t dtype, const void* q_in, int64_t 
     FLP_TRY_HIP(hipGetLastError());
     return FLP_OK;
   };
-  return launch(std::integral_constant<int, 1>{});
+  const int64_t bytes = 2 * (int64_t)n_tokens * (a.n_q + a.n_kv) * head_dim * eb;
+  return bytes > (int64_t)32 << 20 ? launch(std::integral_constant<int, 4>{}) : launch(std::integral_constant<int, 1>{});
 }
 
 extern "C" flp_status fll_silu_mul(int32_t dtype, const void* gate, int64_t ld_gate, const void* up, int64_t ld_up,
