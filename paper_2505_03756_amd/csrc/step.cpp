@@ -171,6 +171,8 @@ bool inline_records(const AttnLaunch& l) {
 constexpr int kMaxPieces = 64;
 constexpr int kWaveSlots = 512, kTileSlots = 256;      // workgroups of four waves, and of the tiled kernel, that the chip holds at once
 
+// The pieces of a launch's contexts, `piece` tiles at most, and the places that follow from them; tiles, groups: of each record, tiles
+// of its context and workgroups that its rows take
 void cut(AttnLaunch& l, int64_t piece, int n_kv, const int64_t* tiles, const int64_t* groups, int64_t* parts) {
   l.units = l.units_each = 0;
   l.merge_rows = 0;
@@ -190,6 +192,25 @@ void cut(AttnLaunch& l, int64_t piece, int n_kv, const int64_t* tiles, const int
   }
 }
 
+// Which kernel takes which sequences, how a workgroup's waves divide the work, and where contexts are cut.  Times below: whole calls, us.
+//
+// Tiled kernel or few rows.  The first reads K and V once for 256 rows, the second once for 16 (from L2 after the first time).  Few rows / tiled,
+// 64 / 8 heads, bf16 trees: 48 sequences of 2000 positions, 48 tokens 674 / 187; 14 of 280, 5 to 15 tokens 17.3 / 13.0; one of 700, 16
+// tokens 12.4 / 20; in 8 bits 48 of 1000, 16 tokens 72 / 55, one of 2000, 32 tokens 17 / 26, and with 40 heads of their own, 56 of 600, 6 to 11
+// tokens 58 / 152.  So: from 17 rows on (8 bits, where the second kernel reads half as much: 65), where there is enough of it, and not for
+// short contexts of few rows (169 of 60, 3 to 9 tokens 36 / 49; 124 of 19 to 191, 3 to 22 tokens 60 / 46).  One launch where either kind
+// of sequence is few: 15 of 192 to 1992, 8 to 27 tokens, 32 heads: few rows 55, tiled 57, both kernels 88.
+//
+// Few rows: waves of a workgroup on slices of a context / on heads / on row tiles.  248 single tokens over 28 positions, 40 heads 111 / 50 / 123; 70
+// over 490, 32 heads 52 / 58 / -; 256 over 600, 64 / 8 heads 72 / 69 / 93; 17 sequences of 62 tokens over 210, 40 heads 43 / 43 / 36; 49 of 1
+// to 34 tokens over 2300, 32 heads 187 / - / 247 (most of them fill one row tile).  Eight waves: one token over 2000 positions in 8 bits 15.5,
+// four 16.5.
+//
+// Pieces.  A workgroup alone on its CU fetches 64 bytes a nanosecond; pieces cost the launch that merges them, 6 us.  Whole / pieces of 8 tiles / of
+// 32, one token, 64 / 8 heads, bf16: 600 positions 10.6 / 13.2 / 10.5; 2000 23 / 13.5 / 21; 8000 75 / 15.3 / 22; eight of 8000 87 / 52 / 48.  48 of
+// 1000 fill the chip: 33.5 / 42 / 33.5.  Tiled kernel: a step of a workgroup takes about 1.8 us, what is not in steps about 4; with pieces 5
+// for the launch and the partials' way out and back (520 bytes a row).  Trees of 32 to 64 tokens over 8 to 16 k positions, 64 / 8 heads: pieces
+// of 90 tiles 283, 40 244, 24 265; 16 prompts of 40 heads whole 213, of 32 tiles 255.
 std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, const std::vector<FlpStepSeq>& all, size_t* part_rows) {
   std::vector<AttnLaunch> launches;
   const int n_kv = p->cfg.n_kv_heads, pb = p->cfg.block_tokens * (p->elem_bytes / elem_bytes), run = 64 / elem_bytes;
@@ -197,17 +218,26 @@ std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, cons
   const auto length = [](const FlpStepSeq& r) { return (int64_t)r.prefix + r.n; };
   const auto over = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
   const auto fits = [&](const FlpStepSeq& r) { return over(length(r), pb) <= kMfmaMaxBlocks; };
-  // 16-row tiles of the queries times tiles of the context, over all kv heads, of the sequences with more than `rows` query rows and of the others
-  const auto work = [&](int rows, int64_t (&w)[2]) {
-    w[0] = w[1] = 0;
-    for (const FlpStepSeq& r : all)
-      w[tiles_ok && fits(r) && (int64_t)r.n * G > rows] += over((int64_t)r.n * G, 16) * over(length(r), run) * n_kv;
+  // 16-row tiles of the queries times tiles of the context, over all kv heads, of the sequences with more than `rows` query rows (w[1]) and
+  // of the others; area: of the former, rows times positions of a sequence and kv head, the mean
+  int64_t w[2], area = 0;
+  const auto work = [&](int rows) {
+    int64_t seqs = 0;
+    w[0] = w[1] = area = 0;
+    for (const FlpStepSeq& r : all) {
+      const int64_t R = (int64_t)r.n * G;
+      const bool is = tiles_ok && fits(r) && R > rows;
+      w[is] += over(R, 16) * over(length(r), run) * n_kv;
+      if (!is) continue;
+      area += R * length(r);
+      ++seqs;
+    }
+    if (seqs) area /= seqs;
   };
-  int64_t w[2];
   int from = 16;                                       // sequences with more query rows than that go to the tiled kernel
-  work(from, w);
-  if (elem_bytes == 1 || w[1] < 8 * w[0]) work(from = 64, w);
-  if (w[1] <= (elem_bytes == 1 ? 12000 : 6000))
+  work(from);
+  if (elem_bytes == 1 || w[1] < 8 * w[0]) work(from = 64);
+  if (w[1] <= (elem_bytes == 1 ? 12000 : 6000) || area < 8000)
     from = INT32_MAX;
   else if (w[1] > 8 * w[0])
     from = 0;                                          // what little is left comes along
@@ -217,12 +247,8 @@ std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, cons
   for (int t = 1; t >= 0; --t) {
     AttnLaunch l{};
     l.tiles = t == 1;
-    int64_t rows = 0;
     for (const FlpStepSeq& r : all)
-      if (tiled(r) == l.tiles) {
-        l.recs.push_back(r);
-        rows = std::max<int64_t>(rows, (int64_t)r.n * G);
-      }
+      if (tiled(r) == l.tiles) l.recs.push_back(r);
     if (l.recs.empty()) continue;
     std::stable_sort(l.recs.begin(), l.recs.end(), [&](const FlpStepSeq& x, const FlpStepSeq& y) { return length(x) > length(y); });
     l.head_waves = l.row_waves = 1;
@@ -235,9 +261,9 @@ std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, cons
         steps += x * over(length(r), tile);
       }
       const bool few_steps = waves >= 768 && steps <= 4 * waves;
-      if (rows > 32 && (waves >= 4 * kWaveSlots || few_steps))
+      if (waves >= 3 * n_kv * (int64_t)l.recs.size() && (waves >= 4 * kWaveSlots || few_steps))
         l.row_waves = 4;
-      else if (few_steps || (waves >= 4 * kWaveSlots && steps <= 16 * waves))
+      else if (few_steps || (waves >= 6 * kWaveSlots && steps <= 16 * waves))
         l.head_waves = 4;
     }
     const int per_group = l.tiles ? kMfmaRowsPerItem : 16 * l.row_waves;
