@@ -156,10 +156,11 @@ flp_status flp_paged_prefix_attention(flp_pool* pool, const flp_attn_batch* batc
  * position p of sequence i lives in block block_tables[i][p / pb], slot p % pb, and the limits on lengths go by pb.
  * fp32 pools: FLP_ENOTSUP.
  *
- * These calls (and the tree and accept calls further down) allocate nothing and keep no state, but for attention calls of more than
- * 96 sequences with new tokens or of contexts that are cut into pieces: those need a staging slot or the pool's workspace, and under
- * stream capture they are refused (FLP_ENOTSUP).  All others can be captured into a HIP graph and replayed.  The pool's device must be
- * the current one (FLP_EINVAL). */
+ * These calls (and the tree and accept calls further down) allocate nothing and keep no state, but for attention calls whose batch
+ * needs a staging slot (more than 96 sequences with new tokens) or the pool's workspace (contexts that are cut into pieces over
+ * workgroups, as long ones of small batches are), and tree calls that append K and V of the pool's type: under stream capture
+ * these are refused (FLP_ENOTSUP, nothing enqueued).  All others can be captured into a HIP graph and replayed.  Calls on
+ * several streams owe each other no order but that of the data.  The pool's device must be the current one (FLP_EINVAL). */
 typedef struct {
   const float* k_scale;           /* device float[n_kv_heads], finite and > 0                 */
   const float* v_scale;           /* device float[n_kv_heads], finite and > 0                 */
