@@ -157,7 +157,7 @@ flp_status flp_paged_prefix_attention(flp_pool* pool, const flp_attn_batch* batc
  * fp32 pools: FLP_ENOTSUP.
  *
  * These calls (and the tree and accept calls further down) allocate nothing and keep no state, but for attention calls whose batch
- * needs a staging slot (more than 96 sequences with new tokens) or the pool's workspace (contexts that are cut into pieces over
+ * needs a staging slot (more than 224 sequences with new tokens) or the pool's workspace (contexts that are cut into pieces over
  * workgroups, as long ones of small batches are), and tree calls that append K and V of the pool's type: under stream capture
  * these are refused (FLP_ENOTSUP, nothing enqueued).  All others can be captured into a HIP graph and replayed.  Calls on
  * several streams owe each other no order but that of the data.  The pool's device must be the current one (FLP_EINVAL). */

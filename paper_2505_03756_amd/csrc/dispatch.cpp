@@ -112,9 +112,7 @@ bool append_reads_host(const flp_pool* p, size_t n_units) {
 
 }  // namespace
 
-extern "C" flp_status flp_kv_append(flp_pool* p, const flp_attn_batch* b, void* hip_stream) {
-  FLP_TRY(check_attn_batch(p, b, false, true, "flp_kv_append"));
-  std::lock_guard<std::mutex> lk(p->mu);
+flp_status flp_enqueue_append(flp_pool* p, const flp_attn_batch* b, hipStream_t stream) {
   const std::vector<FlpAppendUnit> units = append_units(b);
   if (units.empty()) return FLP_OK;
   FlpStageSlot* slot = nullptr;
@@ -122,13 +120,19 @@ extern "C" flp_status flp_kv_append(flp_pool* p, const flp_attn_batch* b, void* 
   FLP_TRY(flp_stage_acquire(p, bytes, &slot));
   memcpy(slot->host, units.data(), bytes);
   const bool direct = append_reads_host(p, units.size());
-  flp_status s1 = direct ? FLP_OK : flp_stage_upload(slot, bytes, (hipStream_t)hip_stream);
+  flp_status s1 = direct ? FLP_OK : flp_stage_upload(slot, bytes, stream);
   if (s1 == FLP_OK)
     s1 = flp_launch_kv_append(p->cfg.dtype, p->cfg.head_dim, make_args(p, b),
                               (const FlpAppendUnit*)(direct ? slot->host : slot->dev), (int32_t)units.size(), nullptr, nullptr, 0,
-                              (hipStream_t)hip_stream);
-  flp_status s2 = flp_stage_release(slot, (hipStream_t)hip_stream);
+                              stream);
+  flp_status s2 = flp_stage_release(slot, stream);
   return s1 != FLP_OK ? s1 : s2;
+}
+
+extern "C" flp_status flp_kv_append(flp_pool* p, const flp_attn_batch* b, void* hip_stream) {
+  FLP_TRY(check_attn_batch(p, b, false, true, "flp_kv_append"));
+  std::lock_guard<std::mutex> lk(p->mu);
+  return flp_enqueue_append(p, b, (hipStream_t)hip_stream);
 }
 
 namespace {

@@ -187,6 +187,8 @@ flp_status flp_launch_attn_merge(int dtype, int head_dim, const FlpAttnArgs& a, 
 // the workspace of an attention call that splits, for work on `stream`: a call on another stream waits for the one before it
 // (the caller owes no ordering to calls whose sequences are different ones, and cannot see which of them split)
 flp_status flp_attn_workspace(flp_pool* pool, size_t bytes, hipStream_t stream, void** out);
+// flp_kv_append of a batch that has been checked, with the pool's lock held
+flp_status flp_enqueue_append(flp_pool* pool, const flp_attn_batch* batch, hipStream_t stream);
 
 flp_status flp_launch_attn_mfma(int dtype, const FlpAttnArgs& a, const FlpMfmaItem* items_dev, int32_t n_items,
                                 const FlpAttnUnit* units_dev, hipStream_t stream);
@@ -255,6 +257,10 @@ flp_status flp_launch_attn_step(int dtype, int head_dim, const FlpStepArgs& a, c
 flp_status flp_launch_attn_step_tiles(int dtype, const FlpStepArgs& a, const FlpStepSeq* inline_recs, int64_t n_units, hipStream_t stream);
 // the pieces of a launch of either kind that has merge rows
 flp_status flp_launch_attn_step_merge(int dtype, int head_dim, const FlpStepArgs& a, const FlpStepSeq* inline_recs, hipStream_t stream);
+// how the attention of a batch over an 8-bit cache or of drafted trees runs, for tests: a byte for the launch of few rows, the next for the
+// tiled kernel's; 0 where there is none, otherwise 1, plus 2 where contexts are cut, plus 4 times where the records are (0 the short list, 1
+// the long one, 2 the packed one, 3 staged), plus, of few rows, 16 times waves on heads (1), on row tiles (2) or eight slices (3)
+extern "C" int32_t flp_step_attention_route(const flp_pool* pool, const flp_attn_batch* batch, int32_t kv8);
 constexpr int kAppend8Slots = 32;      // a unit of the 8-bit append: the slots of one such run of positions
 flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpSeqList<kListSeqs>& list, int32_t n_units,
                                  hipStream_t stream);

@@ -169,6 +169,7 @@ bool inline_records(const AttnLaunch& l) {
 }
 
 constexpr int kMaxPieces = 64;
+constexpr int64_t kMaxWaves = (1ll << 26) - 1;         // of a launch: the runtime counts its threads in 32 bits
 constexpr int kWaveSlots = 512, kTileSlots = 256;      // workgroups of four waves, and of the tiled kernel, that the chip holds at once
 
 // The pieces of a launch's contexts, `piece` tiles at most, and the places that follow from them; tiles, groups: of each record, tiles
@@ -317,15 +318,15 @@ std::vector<AttnLaunch> attn_plan(const flp_pool* p, int G, int elem_bytes, cons
   return launches;
 }
 
-// The attention of a batch that has passed the checks; with_append8: K and V of the new tokens are stored in 8 bits before it
-flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, const uint64_t* mask, bool with_append8,
+// The attention of a batch that has passed the checks; with_append: K and V of the new tokens are stored before it
+flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, const uint64_t* mask, bool with_append,
                   const std::vector<FlpStepSeq>& recs, hipStream_t stream, const char* who) {
   std::lock_guard<std::mutex> lk(p->mu);
   size_t part_rows = 0;
   const std::vector<AttnLaunch> launches = attn_plan(p, b->n_q_heads / p->cfg.n_kv_heads, sc ? 1 : p->elem_bytes, recs, &part_rows);
   size_t staged = 0;
   for (const AttnLaunch& l : launches) {
-    if (l.units * p->cfg.n_kv_heads > INT32_MAX || (int64_t)l.merge_rows * b->n_q_heads > INT32_MAX) {
+    if (l.units * p->cfg.n_kv_heads * l.waves > kMaxWaves || (int64_t)l.merge_rows * b->n_q_heads > kMaxWaves) {
       flp_set_error("%s: more rows than one launch takes", who);
       return FLP_ERANGE;
     }
@@ -334,8 +335,10 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
   FlpStageSlot* slot = nullptr;
   FlpStepArgs a = make_args(p, b, sc, sc != nullptr);
   a.mask = mask;
+  const bool append16 = with_append && !sc;            // the pool's own append, whose units are staged
+  if (staged || part_rows || append16) FLP_TRY(refuse_capture(stream, who));
+  if (append16) FLP_TRY(flp_enqueue_append(p, b, stream));
   if (staged || part_rows) {
-    FLP_TRY(refuse_capture(stream, who));
     if (part_rows) {
       void* w = nullptr;
       FLP_TRY(flp_attn_workspace(p, part_rows * b->n_q_heads * (p->cfg.head_dim + 2) * sizeof(float), stream, &w));
@@ -347,7 +350,7 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
       if (!inline_records(l)) to = std::copy(l.recs.begin(), l.recs.end(), to);
   }
   flp_status s = staged ? flp_stage_upload(slot, staged * sizeof(FlpStepSeq), stream) : FLP_OK;
-  if (s == FLP_OK && with_append8) s = append8(p, b, sc, stream);
+  if (s == FLP_OK && with_append && sc) s = append8(p, b, sc, stream);
   const FlpStepSeq* at = slot ? (const FlpStepSeq*)slot->dev : nullptr;
   for (size_t i = 0; i < launches.size() && s == FLP_OK; ++i) {
     const AttnLaunch& l = launches[i];
@@ -386,6 +389,19 @@ flp_status guarded(const char* who, F f) {
 }
 
 }  // namespace
+
+extern "C" int32_t flp_step_attention_route(const flp_pool* p, const flp_attn_batch* b, int32_t kv8) {
+  std::vector<FlpStepSeq> recs;
+  if (check_batch(p, b, nullptr, Call{"flp_step_attention_route", kv8 != 0, false, false, 0}, &recs) != FLP_OK) return -1;
+  size_t part_rows = 0;
+  int32_t route = 0;
+  for (const AttnLaunch& l : attn_plan(p, b->n_q_heads / p->cfg.n_kv_heads, kv8 ? 1 : p->elem_bytes, recs, &part_rows)) {
+    const int place = !inline_records(l) ? 3 : l.recs.size() <= (size_t)kShortList ? 0 : l.merge_rows ? 1 : 2;
+    const int split = l.tiles ? 0 : l.head_waves > 1 ? 1 : l.row_waves > 1 ? 2 : l.waves == 8 ? 3 : 0;
+    route |= (1 | (l.merge_rows ? 2 : 0) | 4 * place | 16 * split) << (l.tiles ? 8 : 0);
+  }
+  return route;
+}
 
 extern "C" int64_t flp_pool_kv8_block_tokens(const flp_pool* p) { return p ? kv8_tokens(p) : 0; }
 
@@ -433,11 +449,7 @@ extern "C" flp_status flp_paged_tree_attention(flp_pool* p, const flp_attn_batch
       return FLP_EINVAL;
     }
     FLP_TRY(check_device(p, who));
-    if (append && !sc) {                               // the pool's own append, whose units are staged
-      FLP_TRY(refuse_capture((hipStream_t)hip_stream, who));
-      FLP_TRY(flp_kv_append(p, b, hip_stream));
-    }
-    return attend(p, b, sc, tree_mask, append && sc, recs, (hipStream_t)hip_stream, who);
+    return attend(p, b, sc, tree_mask, append, recs, (hipStream_t)hip_stream, who);
   });
 }
 
