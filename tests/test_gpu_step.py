@@ -4,9 +4,11 @@ float64 oracle.
 Tolerances.  A result is rounded once, by half a step: HALF * |value|.  Before that, attention's scores are sums of d products in fp32
 (off by at most d 2^-24 times the sum of their sizes, `worst`), which moves a weight by as much relative to itself, exp2 by a few
 2^-23, the sums of weights by length * 2^-24 and the pieces that a 16-bit weight is held in by 2^-16 (bf16) or less; a weighted mean
-of values of size vmax moves by at most twice the weights' relative change times vmax.  Sequences of more than 64 query rows per kv head
-(16-bit types, head_dim 128) have their weights rounded once to the type of V, fp16 over an 8-bit cache, and summed as rounded: with
-weights w (1 + e), |e| <= HALF, the mean moves by at most 2 HALF vmax."""
+of values of size vmax moves by at most twice the weights' relative change times vmax.  In calls that the tiled kernel has a part in
+weights may be rounded once to the type of V, fp16 over an 8-bit cache, and summed as rounded: with weights w (1 + e), |e| <= HALF, the
+mean moves by at most 2 HALF vmax."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -96,13 +98,13 @@ class Setup:
         got = self.out.double().cpu().numpy()
         assert (got[self.T:] == 7).all(), "rows behind the last sequence were written"
         q = wl.dequantize(self.q, self.dtype)
+        once = any(x.startswith("tiles") for x in self.routes())
         for i, (p, n) in enumerate(self.seqs):
             lo, hi = self.cu[i], self.cu[i + 1]
             if lo == hi:
                 continue
             k, v = self.values(image, i)
             ref, worst, vmax = so.attention(q[lo:hi], k, v, sees(i), scale)
-            once = self.dtype != "f32" and self.d == 128 and n * self.nq // self.nkv > 64
             pieces = 0 if self.dtype == "f32" else 2 * HALF["f16" if self.kv8 else self.dtype] if once else 2.0 ** -16
             tol = HALF[self.dtype] * np.abs(ref) + TINY[self.dtype] + vmax * (
                 2 * (self.d * 2.0 ** -24 * worst + 2.0 ** -20 + (p + n) * 2.0 ** -24) + pieces)[..., None]
@@ -115,6 +117,13 @@ class Setup:
     def prefix8(self, append=False, **kw):
         more = dict(k_new=self.t["k_new"], v_new=self.t["v_new"]) if append else {}
         self.pool.paged_prefix_attention8(self.t["q"], self.out, self.t["ks"], self.t["vs"], *self.where, n_q_heads=self.nq, **more, **kw)
+
+    def routes(self):
+        """The launches of the batch's attention: kernel, what its waves are side by side on, whether contexts are cut, where the records are."""
+        b, keep = self.pool._attn_batch(*self.where, self.tables.shape[1], self.nq, None, None, None, None, 0.0)
+        code = flpool.load().flp_step_attention_route(self.pool._h, C.byref(b), int(self.kv8))
+        return [" ".join(x for x in (("rows", "tiles")[i], ("", "heads", "row tiles", "eight")[c >> 4], "cut" * (c >> 1 & 1),
+                                     ("", "long", "packed", "staged")[c >> 2 & 3]) if x) for i, c in enumerate((code & 255, code >> 8)) if c]
 
     def tree(self, masks, append=False, **kw):
         more = dict(k_new=self.t["k_new"], v_new=self.t["v_new"]) if append else {}
@@ -273,6 +282,113 @@ def test_tree_keeps_hidden_values_apart(kind, heads):
     s.check(lambda i: so.tree(*s.seqs[i], masks[i]))
 
 
+# ---------------------------------------------------------------------------------------------------------- every way to run them
+def spread(n, lo, hi, new, seed=0):
+    """n sequences: prefixes of lo .. hi, the new tokens in turns."""
+    r = np.random.default_rng(seed)
+    return [(int(r.integers(lo, hi + 1)), new[i % len(new)]) for i in range(n)]
+
+
+WAYS = [  # name, heads, sequences, the launches in 16 bits, and in 8
+    ("few", (4, 4, 128), spread(80, 0, 300, [1]), ["rows packed"], ["rows packed"]),
+    ("few, cut", (4, 2, 64), [(2300, 2), (40, 3)], ["rows cut"], ["rows cut"]),
+    ("few, cut, long list", (1, 1, 128), [(4000, 1)] + spread(40, 0, 70, [1, 2]), ["rows cut long"], ["rows cut long"]),
+    ("few, cut, staged", (2, 1, 128), [(4000, 3)] + spread(120, 0, 70, [1, 2, 0]) + spread(30, 0, 70, [1]), ["rows cut staged"], ["rows cut staged"]),
+    ("heads", (10, 5, 64), spread(270, 0, 60, [1, 2, 0, 3, 1]), ["rows heads packed"], ["rows heads packed"]),
+    ("heads, staged", (10, 5, 64), spread(250, 0, 90, [1]), ["rows heads staged"], ["rows heads staged"]),
+    ("row tiles", (16, 4, 64), spread(24, 0, 50, [33, 64, 13, 50, 1]), ["rows row tiles packed"], ["rows row tiles packed"]),
+    ("row tiles, few sequences", (64, 4, 64), spread(8, 0, 50, [33, 64, 13, 50]), ["rows row tiles"], ["rows row tiles"]),
+    ("tiles", (64, 4, 128), [(0, 64), (700, 19)] + spread(6, 400, 700, [64, 57]), ["tiles"], ["tiles"]),
+    ("tiles, packed", (32, 4, 128), [(0, 64), (0, 40), (1, 63)] + spread(27, 0, 500, [64, 40, 57, 1]), ["tiles packed"], ["tiles packed"]),
+    ("tiles, staged", (8, 1, 128), spread(230, 0, 200, [64, 40]), ["tiles staged"], ["tiles staged"]),
+    ("tiles, cut", (64, 2, 128), [(6001, 64), (500, 19)], ["tiles cut"], ["tiles cut"]),
+    ("tiles, cut, long list", (16, 1, 128), spread(12, 1500, 2100, [64, 39]), ["tiles cut long"], ["tiles cut long"]),
+    ("both", (32, 4, 128), spread(16, 300, 700, [64]) + spread(70, 300, 900, [1, 2]), ["rows packed", "tiles packed"], ["rows packed", "tiles packed"]),
+]
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16", "f16 8", "bf16 8"])
+@pytest.mark.parametrize("bt", [16, 32])
+@pytest.mark.parametrize("way", WAYS, ids=lambda w: w[0])
+def test_trees_every_way(way, bt, kind):
+    """Trees by every launch that the plan knows, tokens without any bit and K and V that are not finite and hidden from some rows among them."""
+    _, heads, seqs, in16, in8 = way
+    dtype, kv8 = kind.split()[0], kind.endswith("8")
+    s = Setup(dtype, *heads, seqs, kv8=kv8, bt=bt, seed=30)
+    r = np.random.default_rng(31)
+    masks = [random_tree(r, n) for _, n in seqs]
+    bits = [127] * 3 if kv8 else wl.quantize(np.array([np.nan, np.inf, -np.inf], np.float32), dtype)
+    flat = s.image.reshape(-1)
+    for i, (p, n) in enumerate(seqs):
+        if i % 3 == 0 and n > 1:
+            for x in range(3):
+                at = so.pages(s.image, s.tables[i], [p + int(r.integers(0, n))], s.nkv, s.d, s.pb, 1)[0]
+                flat[at[:, 5 * x::31]] = bits[x]
+        if i % 4 == 0 and n > 1:
+            flat[so.pages(s.image, s.tables[i], [p + n - 1], s.nkv, s.d, s.pb, 0)[0, -1, 9]] = bits[0]
+    s.device()
+    assert s.routes() == (in8 if kv8 else in16)
+    s.tree(masks)
+    s.check(lambda i: so.tree(*s.seqs[i], masks[i]))
+    assert same(s.now(), s.image)
+
+
+PROMPTS = [
+    ("tiles", (8, 8, 128), [(1000, 700), (0, 800), (333, 600), (77, 65), (10, 1)], ["tiles"]),
+    ("tiles, packed", (16, 2, 128), spread(24, 0, 500, [350, 164, 397, 1]), ["tiles packed"]),
+    ("tiles, cut", (16, 2, 128), [(3000, 300)], ["tiles cut"]),
+    ("tiles, cut, from nothing", (16, 1, 128), [(0, 1500)], ["tiles cut"]),
+    ("row tiles", (16, 4, 64), spread(24, 0, 100, [33, 64, 13, 90, 1]), ["rows row tiles packed"]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("bt", [16, 32])
+@pytest.mark.parametrize("way", PROMPTS, ids=lambda w: w[0])
+def test_prompts_every_way(way, bt, dtype):
+    """Prompts over the 8-bit cache, NaN in V of a few new tokens (the rows before them do not see it)."""
+    _, heads, seqs, launches = way
+    s = Setup(dtype, *heads, seqs, kv8=True, bt=bt, seed=32)
+    for i, (p, n) in enumerate(seqs):
+        if i % 2 == 0 and n > 30:
+            for x, at in enumerate((n // 3, n - 2)):
+                s.image.reshape(-1)[so.pages(s.image, s.tables[i], [p + at], s.nkv, s.d, s.pb, 1)[0, :, 3 + x::17]] = 127 + 128 * x
+    s.device()
+    assert s.routes() == launches
+    s.prefix8()
+    s.check(lambda i: so.causal(*s.seqs[i]))
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16 8"])
+def test_blocks_far_into_a_large_pool(kind):
+    """Blocks more than 2^32 bytes behind the pool's base: stored, read by both kernels and moved."""
+    dtype, kv8 = kind.split()[0], kind.endswith("8")
+    seqs = spread(8, 0, 700, [64, 41, 17])
+    s = Setup(dtype, 32, 4, 128, seqs, kv8=kv8, seed=33)
+    r = np.random.default_rng(34)
+    masks = [random_tree(r, n) for _, n in seqs]
+    image = s.append_oracle()
+    s.device()
+    block = s.image[0].nbytes
+    before = (5 << 30) // block
+    big = torch.zeros((before + s.n_blocks) * block, dtype=torch.uint8, device="cuda")
+    big[before * block:] = s.t["image"].view(torch.uint8).reshape(-1)
+    s.t["image"] = big[before * block:]
+    far = np.where(s.tables >= 0, s.tables + before, -1).astype(np.int32)
+    s.pool = flpool.Pool(dtype, 4, 128, before + s.n_blocks, 0, block_tokens=16, dev=big)
+    s.where = (s.cu, s.P, up(far))
+    s.tree(masks, append=True)
+    assert same(s.now().reshape(-1), image.reshape(-1))
+    s.check(lambda i: so.tree(*s.seqs[i], masks[i]), image)
+    taken, path = np.zeros(len(seqs), np.int32), np.full(s.T, -1, np.int32)
+    for i, (p, n) in enumerate(seqs):
+        taken[i] = n // 2
+        path[s.cu[i]:s.cu[i] + taken[i]] = np.sort(r.choice(n, taken[i], replace=False))
+        so.accept(image, s.tables[i], p, n, int(taken[i]), path[s.cu[i]:s.cu[i + 1]], s.nkv, s.d, s.pb)
+    s.pool.kv_accept(up(taken), up(path), *s.where, kv8=kv8)
+    assert same(s.now().reshape(-1), image.reshape(-1)) and not bool(big[:before * block].any())
+
+
 # ---------------------------------------------------------------------------------------------------------- accepted paths
 @pytest.mark.parametrize("bt", [16, 32])
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "f16 8"])
@@ -289,6 +405,22 @@ def test_accept(kind, heads, bt):
         if m > 3 and i % 5 == 0:                           # an entry that is none ends the path; more taken than there are
             path[s.cu[i] + 2] = n if i % 2 else -1
             taken[i] = n + 7
+        so.accept(want, s.tables[i], p, n, int(taken[i]), path[s.cu[i]:s.cu[i + 1]], s.nkv, s.d, s.pb)
+    s.device()
+    s.pool.kv_accept(up(taken), up(path), *s.where, kv8=s.kv8)
+    assert same(s.now(), want)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16 8"])
+def test_accept_of_long_paths(kind):
+    """More tokens than a tree has: paths over many blocks, some of which the first 64 table entries do not hold."""
+    r = np.random.default_rng(18)
+    seqs = [(7, 300), (0, 2500), (30, 90), (5, 0)]
+    s = Setup(kind.split()[0], 4, 2, 64, seqs, kv8=kind.endswith("8"), seed=19)
+    taken, path, want = np.array([200, 1200, 90, 1], np.int32), np.full(s.T, -1, np.int32), s.image.copy()
+    for i, (p, n) in enumerate(seqs):
+        m = min(n, int(taken[i]))
+        path[s.cu[i]:s.cu[i] + m] = np.sort(r.choice(n, m, replace=False)) if n else []
         so.accept(want, s.tables[i], p, n, int(taken[i]), path[s.cu[i]:s.cu[i + 1]], s.nkv, s.d, s.pb)
     s.device()
     s.pool.kv_accept(up(taken), up(path), *s.where, kv8=s.kv8)
