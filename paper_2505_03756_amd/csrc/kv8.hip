@@ -19,15 +19,21 @@ __device__ __forceinline__ float quotient(float x, float s, float r) {
   return x != x ? x : copysignf(q, x);
 }
 
-// Workgroups of K and workgroups of V per unit of 32 slots and 1024 elements of a token's row; a thread owns 8 channels of 16 slots, and all
-// its reads are on their way together.  V is turned in registers into the channels' 16-byte half runs of the transposed layout; the two
-// halves of a run come from one workgroup.  A unit that covers part of its run (the ends of a sequence's new tokens) merges its
+// Workgroups of K and workgroups of V per unit of 32 slots and 64 Q elements of a token's row; a thread owns 8 channels of Q slots, and all
+// its reads are on their way together.  V is turned in registers into Q bytes of each channel's run of the transposed layout; the
+// parts of a run come from one workgroup.  A unit that covers part of its run (the ends of a sequence's new tokens) merges its
 // slots into the words already there, which belong to this sequence alone; units of one or two slots (a decode batch) store
-// single bytes, and are bound by these: 32 bytes apart, a sector each.
-template <typename S, int D, int N>
+// single bytes of V, neighbouring lanes on neighbouring channels.
+//
+// Q = 16: bound by memory; 32 prompts of 128 to 512 tokens, 40 heads, 303 MB 68 us, 4.5 TB/s (Q = 4: 88).  256 single tokens of 32
+// heads 11.5 us, a million sectors of 32 bytes written in part (with eight channels per thread 12.6).  Q = 4: four times as many threads, where a
+// workgroup's 16 x 8 conversions are what a launch waits for: 16 tokens of 8 heads 7.5 -> 4.0 us, 24 x 64 tokens 8.8 -> 6.8, 512 of 40
+// heads 8.9 -> 6.7; 2 x 512 (340 workgroups of the other kind) 11.5 either way.
+template <typename S, int D, int Q, int N>
 __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqList<N> list) {
   typedef typename S::storage ST;
-  constexpr int SL = kAppend8Slots;
+  typedef uint32_t words __attribute__((ext_vector_type(Q / 4)));
+  constexpr int SL = kAppend8Slots, COLS = 64 * Q;     // elements of a token's row that a workgroup takes
   const int row = a.n_kv * D, u = blockIdx.x;
   const bool is_v = blockIdx.y & 1;
   int rec = -1;                                        // the last sequence whose first unit is not behind u
@@ -46,8 +52,25 @@ __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqLi
   const int slot0 = run * SL & (a.pb - 1);
   const int64_t blk = a.tables[(int64_t)(list.seq0 + rec) * a.max_blocks + run * SL / a.pb];
   uint8_t* const base = a.pool + blk * a.block_bytes;
-  const int e0 = (blockIdx.y >> 1) * 1024 + (threadIdx.x & 127) * 8, h = threadIdx.x >> 7;
-  if (e0 >= row || s1 <= 16 * h || s0 >= 16 * h + 16) return;
+  const int c0 = (blockIdx.y >> 1) * COLS;
+  if (is_v && s1 - s0 <= 2) {
+    for (int s = s0; s < s1; ++s) {
+      const ST* const src = reinterpret_cast<const ST*>(a.v_new) + (t0 + s) * row;
+      ST x[COLS / 256];
+#pragma unroll
+      for (int j = 0; j < COLS / 256; ++j) x[j] = src[min(c0 + 256 * j + (int)threadIdx.x, row - 1)];
+#pragma unroll
+      for (int j = 0; j < COLS / 256; ++j) {
+        const int e = c0 + 256 * j + threadIdx.x;
+        if (e >= row) break;
+        const float scale = a.v_scale[e / D], q = quotient(S::to_float(x[j]), scale, 1.f / scale);
+        base[(int64_t)(row + e) * a.pb + slot0 + s] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(q, q, 0, false);
+      }
+    }
+    return;
+  }
+  const int e0 = c0 + (threadIdx.x % (8 * Q)) * 8, h = threadIdx.x / (8 * Q);
+  if (e0 >= row || s1 <= Q * h || s0 >= Q * h + Q) return;
   const int g = e0 / D;
   const float scale = is_v ? a.v_scale[g] : a.k_scale[g], r = 1.f / scale;
   const ST* const src = reinterpret_cast<const ST*>(is_v ? a.v_new : a.k_new) + t0 * row + e0;
@@ -65,50 +88,43 @@ __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqLi
     w.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[6], f[7], w.y, true);
     return w;
   };
-  if (s1 - s0 <= 2) {
-    for (int s = s0 > 16 * h ? s0 : 16 * h; s < s1 && s < 16 * h + 16; ++s) {
-      const uint2 w = bytes8(*reinterpret_cast<const u32x4*>(src + (int64_t)s * row));
-      if (!is_v) {
-        *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = w;
-        continue;
-      }
-#pragma unroll
-      for (int c = 0; c < 8; ++c) dst[(int64_t)c * a.pb + s] = (uint8_t)((c < 4 ? w.x : w.y) >> (8 * (c & 3)));
-    }
+  if (s1 - s0 <= 2) {                                  // K
+    for (int s = s0 > Q * h ? s0 : Q * h; s < s1 && s < Q * h + Q; ++s)
+      *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = bytes8(*reinterpret_cast<const u32x4*>(src + (int64_t)s * row));
     return;
   }
-  u32x4 x[16];
+  u32x4 x[Q];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int s = 16 * h + i;
+  for (int i = 0; i < Q; ++i) {
+    const int s = Q * h + i;
     if (s >= s0 && s < s1) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (int64_t)s * row));
   }
-  uint2 by_slot[16];
+  uint2 by_slot[Q];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int s = 16 * h + i;
+  for (int i = 0; i < Q; ++i) {
+    const int s = Q * h + i;
     by_slot[i] = bytes8(x[i]);
     if (!is_v && s >= s0 && s < s1) *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = by_slot[i];
   }
   if (!is_v) return;
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
-    u32x4* const at = reinterpret_cast<u32x4*>(dst + (int64_t)c * a.pb + 16 * h);
-    u32x4 w;
+    words* const at = reinterpret_cast<words*>(dst + (int64_t)c * a.pb + Q * h);
+    words w;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < Q / 4; ++q) {
       uint32_t b = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) b |= (((c < 4 ? by_slot[4 * q + i].x : by_slot[4 * q + i].y) >> (8 * (c & 3))) & 0xffu) << (8 * i);
       w[q] = b;
     }
-    if (s0 > 16 * h || s1 < 16 * h + 16) {
-      const u32x4 old = *at;
+    if (s0 > Q * h || s1 < Q * h + Q) {
+      const words old = *at;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < Q / 4; ++q) {
         uint32_t mask = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mask |= 16 * h + 4 * q + i >= s0 && 16 * h + 4 * q + i < s1 ? 0xffu << (8 * i) : 0u;
+        for (int i = 0; i < 4; ++i) mask |= Q * h + 4 * q + i >= s0 && Q * h + 4 * q + i < s1 ? 0xffu << (8 * i) : 0u;
         w[q] = (w[q] & mask) | (old[q] & ~mask);
       }
     }
@@ -116,7 +132,8 @@ __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqLi
   }
 }
 
-// One workgroup per (sequence, kv head).  Bound by latency: the path, its length and the blocks that the new tokens lie in are requested
+// One workgroup per (sequence, kv head).  Bound by latency (one path of 16 tokens, 8 heads 4.7 us) and, in large batches, by the lines of V
+// that the paths' elements lie in, nearly all of the new tokens' blocks (128 paths, 40 heads 24 us): the path, its length and the blocks that the new tokens lie in are requested
 // together, then 32 places of the path at a time are read, K 16 bytes and V an element per access with neighbouring threads on
 // neighbouring places of a channel, and stored behind a barrier.  A place is never behind the token that comes to it, so what is
 // stored for these places is not read for later ones.
@@ -207,14 +224,20 @@ void with_list(const FlpSeqList<kListSeqs>& list, F launch) {
 flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, const FlpSeqList<kListSeqs>& list, int32_t n_units,
                                  hipStream_t stream) {
   if (n_units <= 0) return FLP_OK;
-  const dim3 grid((unsigned)n_units, 2 * (unsigned)((a.n_kv * head_dim + 1023) / 1024));
+  const int row = a.n_kv * head_dim, wide = 2 * ((row + 1023) / 1024);
+  const bool few = (int64_t)n_units * wide < 256;      // less than a workgroup for every CU
+  const dim3 grid((unsigned)n_units, few ? 2 * (unsigned)((row + 255) / 256) : (unsigned)wide);
   with_list(list, [&](const auto& l) {
     constexpr int N = sizeof(l.prefix) / sizeof(int32_t);
     const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, l); };
-    if (dtype == FLP_F16)
-      head_dim == 64 ? launch(kv_append8_kernel<F16, 64, N>) : launch(kv_append8_kernel<F16, 128, N>);
-    else
-      head_dim == 64 ? launch(kv_append8_kernel<BF16, 64, N>) : launch(kv_append8_kernel<BF16, 128, N>);
+    const auto by_size = [&](auto q) {
+      constexpr int Q = decltype(q)::value;
+      if (dtype == FLP_F16)
+        head_dim == 64 ? launch(kv_append8_kernel<F16, 64, Q, N>) : launch(kv_append8_kernel<F16, 128, Q, N>);
+      else
+        head_dim == 64 ? launch(kv_append8_kernel<BF16, 64, Q, N>) : launch(kv_append8_kernel<BF16, 128, Q, N>);
+    };
+    few ? by_size(std::integral_constant<int, 4>{}) : by_size(std::integral_constant<int, 16>{});
   });
   FLP_TRY_HIP(hipGetLastError());
   return FLP_OK;
