@@ -21,7 +21,12 @@
 // A workgroup is four waves, eight in small launches.  Where the launch has enough of them they are independent, side by side on row tiles
 // of a (sequence, kv head), which then read the same K and V at about the same time, or on kv heads; otherwise they take slices of the
 // context, merged in LDS.  Contexts of the smallest launches are cut into pieces over workgroups as well, because one CU
-// fetches no more than 64 bytes a nanosecond; a second launch merges them in piece order.
+// fetches no more than 64 bytes a nanosecond; a second launch merges them in piece order.  For the same reason launches of up to
+// half a workgroup per CU whose contexts are whole give each workgroup a part of V's channels and all of K (launch_kind).
+//
+// Bound by memory: 128 single tokens over 512 to 4096 positions, 32 heads, 8 bits, 2.48 GB: 420 us, 5.9 TB/s; small calls by the trips to
+// memory one after the other (arguments, block table, K and V) and by what a CU fetches: one token over 300 positions of 32 heads,
+// 8 bits, 7.6 us; a tree of 16 tokens over 700, 64 / 8 heads, bf16, 12.1 us.
 //
 // Infinities and NaN in V reach the rows that see them and no others: in the tiles where some row does not see everything, and in
 // all tiles of 16-bit V, values that are not finite are replaced by zero, and whether a row sees one is counted with products of
@@ -105,14 +110,14 @@ __device__ __forceinline__ float got(float v, int) { return v; }
 __device__ __forceinline__ float got(h16x8 v, int e) { return (float)v[e]; }
 __device__ __forceinline__ float got(b16x8 v, int e) { return (float)v[e]; }
 
-// W waves per workgroup; List: the records in the arguments
-template <typename S, int D, bool KV8, int W, typename List>
+// W waves per workgroup; VS workgroups side by side on channels of V; List: the records in the arguments
+template <typename S, int D, bool KV8, int W, int VS, typename List>
 __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, List list) {
   typedef Kind<S, KV8> C;
   typedef typename C::kvec kvec;
   typedef typename C::vvec vvec;
   typedef typename S::storage ST;
-  constexpr int RUN = 16 / C::ES, TP = 4 * RUN, NT = RUN / 4, KC = D * C::ES / 64, CT = D / 16, STEPS = C::STEPS;
+  constexpr int RUN = 16 / C::ES, TP = 4 * RUN, NT = RUN / 4, KC = D * C::ES / 64, CT = D / 16 / VS, STEPS = C::STEPS;
   constexpr int VE = RUN / STEPS;                      // positions of a lane's run that one step of the second product takes
   constexpr uint32_t ALL = (1u << RUN) - 1;
   __shared__ f32x4 merge_o[W][CT][64];
@@ -123,8 +128,9 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // waves side by side on kv heads, within a head on row tiles, and within those on slices of the context
   const int hw = a.head_waves, rw = a.row_waves, per_head = W / hw, kw = per_head / rw;
-  const int head_groups = (a.n_kv + hw - 1) / hw, u = blockIdx.x / head_groups;
-  const int own_head = (blockIdx.x - u * head_groups) * hw + wave / per_head, in_head = wave % per_head;
+  const int head_groups = (a.n_kv + hw - 1) / hw, ub = blockIdx.x / head_groups, u = ub / VS;
+  const int ch0 = (ub - u * VS) * (D / VS);            // the workgroup's first channel
+  const int own_head = (blockIdx.x - ub * head_groups) * hw + wave / per_head, in_head = wave % per_head;
   const int g = own_head < a.n_kv ? own_head : a.n_kv - 1;
   const FlpStepSeq rec = flp_step_record(a, list, u);
   const int G = a.n_h / a.n_kv, R = rec.n * G, P = rec.prefix, L = P + rec.n;
@@ -162,7 +168,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
   };
   const auto load_v = [&](int tile, int32_t blk) {
     const int slot = run_of(tile, lh) & (pb - 1);
-    const uint8_t* p = a.pool + (int64_t)blk * a.block_bytes + ((int64_t)a.n_kv * pb * D + (int64_t)(g * D + lr) * pb + slot) * C::ES;
+    const uint8_t* p = a.pool + (int64_t)blk * a.block_bytes + ((int64_t)a.n_kv * pb * D + (int64_t)(g * D + ch0 + lr) * pb + slot) * C::ES;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) vr[ct] = *reinterpret_cast<const u32x4*>(p + (int64_t)16 * ct * pb * C::ES);
   };
@@ -405,7 +411,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
   const float inv = vs / total;
   const int64_t prow = (int64_t)rec.part0 + (int64_t)tok * rec.pieces + piece;
   float* const pp = a.partials + (prow * a.n_h + (g * G + (rc - tok * G))) * (D + 2);
-  if (r < R && rec.pieces > 1 && lh == 0 && slice == 0) *reinterpret_cast<float2*>(pp) = make_float2(M * c, total);
+  if (r < R && rec.pieces > 1 && lh == 0 && slice == 0 && ch0 == 0) *reinterpret_cast<float2*>(pp) = make_float2(M * c, total);
 #pragma unroll 1
   for (int ct = slice; ct < CT; ct += kw) {
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -418,12 +424,12 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
     }
     if (r >= R) continue;
     if (rec.pieces > 1) {
-      float2* const d2 = reinterpret_cast<float2*>(pp + 2 + 16 * ct + 4 * lh);
+      float2* const d2 = reinterpret_cast<float2*>(pp + 2 + ch0 + 16 * ct + 4 * lh);
       d2[0] = make_float2(o[0] * vs, o[1] * vs);
       d2[1] = make_float2(o[2] * vs, o[3] * vs);
       continue;
     }
-    ST* const op = reinterpret_cast<ST*>(a.out) + rowoff + 16 * ct + 4 * lh;
+    ST* const op = reinterpret_cast<ST*>(a.out) + rowoff + ch0 + 16 * ct + 4 * lh;
     ST e[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) e[i] = S::from_float(nothing ? 0.f : o[i] * inv);
@@ -483,14 +489,27 @@ __global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, Lis
 }
 
 template <typename S, int D>
-void launch_kind(const FlpStepArgs& a, const FlpStepSeq* recs, int waves, unsigned grid, hipStream_t stream) {
+void launch_kind(const FlpStepArgs& a, const FlpStepSeq* recs, int waves, unsigned groups, hipStream_t stream) {
   flp_with_records(a, recs, [&](const auto& list) {
     typedef typename std::decay<decltype(list)>::type L;
-    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * waves), 0, stream, a, list); };
+    const auto launch = [&](auto kernel, int parts = 1) {
+      hipLaunchKernelGGL(kernel, dim3(groups * parts), dim3(64 * waves), 0, stream, a, list);
+    };
+    const auto by_waves = [&](auto kv8) {
+      constexpr bool KV8 = decltype(kv8)::value;
+      if (waves == 4) return launch(attn_step_kernel<S, D, KV8, 4, 1, L>);
+      // Workgroups on parts of V's channels, as many as leave one for each CU.  Whole / 2 / 4 parts, us: one token over 300 positions, 32 heads,
+      // bf16 9.0 / - / 8.0; 16 over 700, 64 / 8 heads 13.3 / - / 12.1; 16 over 300, fp32 15.7 / - / 12.8; 128 workgroups: four tokens over
+      // 700, 32 heads 16.6 / 15.0 / 18.5; 200: three times 16 over 700, 64 / 8 heads 14.9 / 23.8 / 25.
+      if constexpr (std::is_same<L, FlpStepList<kShortList>>::value) {
+        if (groups <= 64) return launch(attn_step_kernel<S, D, KV8, 8, 4, L>, 4);
+        if (groups <= 128) return launch(attn_step_kernel<S, D, KV8, 8, 2, L>, 2);
+      }
+      launch(attn_step_kernel<S, D, KV8, 8, 1, L>);
+    };
     if constexpr (!std::is_same<S, F32>::value)
-      if (a.k_scale)
-        return waves == 8 ? launch(attn_step_kernel<S, D, true, 8, L>) : launch(attn_step_kernel<S, D, true, 4, L>);
-    waves == 8 ? launch(attn_step_kernel<S, D, false, 8, L>) : launch(attn_step_kernel<S, D, false, 4, L>);
+      if (a.k_scale) return by_waves(std::true_type());
+    by_waves(std::false_type());
   });
 }
 

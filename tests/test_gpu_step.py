@@ -175,6 +175,15 @@ def test_append8(dtype, heads, bt):
     assert np.array_equal((got & 127) == 127, nan) and np.array_equal(got[~nan], want[~nan])
 
 
+@pytest.mark.parametrize("bt", [16, 32])
+@pytest.mark.parametrize("heads", [(8, 2, 128), (40, 40, 128), (5, 5, 64)])
+def test_append8_of_large_batches(heads, bt):
+    """Launches with a workgroup for every CU: runs that are whole and cut, single slots, rows that end inside a workgroup's channels."""
+    s = Setup("bf16", *heads, ENDS * 14 + [(5, 1)] * 40 + [(31, 2)] * 9, kv8=True, bt=bt, seed=35).device()
+    s.pool.kv_append8(s.t["k_new"], s.t["v_new"], s.t["ks"], s.t["vs"], *s.where)
+    assert same(s.now(), s.append_oracle())
+
+
 def test_append8_of_many_sequences_and_scales():
     """More sequences than travel in a launch's arguments; quotients of many scales, ties among them."""
     r = np.random.default_rng(5)
