@@ -20,20 +20,24 @@ __device__ __forceinline__ float quotient(float x, float s, float r) {
 }
 
 // Workgroups of K and workgroups of V per unit of 32 slots and 64 Q elements of a token's row; a thread owns 8 channels of Q slots, and all
-// its reads are on their way together.  V is turned in registers into Q bytes of each channel's run of the transposed layout; the
-// parts of a run come from one workgroup.  A unit that covers part of its run (the ends of a sequence's new tokens) merges its
-// slots into the words already there, which belong to this sequence alone; units of one or two slots (a decode batch) store
-// single bytes of V, neighbouring lanes on neighbouring channels.
+// its reads are on their way together.  V is turned in registers into Q bytes of each channel's run of the transposed layout; whole runs
+// leave by way of LDS, neighbouring lanes side by side in memory.  A unit that covers part of its run (the ends of a sequence's new tokens)
+// merges its slots into the words already there, which belong to this sequence alone; units of one or two slots (a decode batch)
+// store single bytes of V, neighbouring lanes on neighbouring channels.
 //
-// Q = 16: bound by memory; 32 prompts of 128 to 512 tokens, 40 heads, 303 MB 68 us, 4.5 TB/s (Q = 4: 88).  256 single tokens of 32
-// heads 11.5 us, a million sectors of 32 bytes written in part (with eight channels per thread 12.6).  Q = 4: four times as many threads, where a
-// workgroup's 16 x 8 conversions are what a launch waits for: 16 tokens of 8 heads 7.5 -> 4.0 us, 24 x 64 tokens 8.8 -> 6.8, 512 of 40
-// heads 8.9 -> 6.7; 2 x 512 (340 workgroups of the other kind) 11.5 either way.
+// Q = 16: bound by memory; 32 prompts of 300 tokens, 40 heads, 295 MB 61 us, 4.8 TB/s (each thread storing its own runs 66 us; 500 drafts of 40
+// tokens, 4 heads, whose runs are cut, 33 and 31).  Where runs follow one another and exceed the caches they are stored past these: 20
+// prompts of 2000 tokens 264 -> 219 us (32 of 300 the same; blocks of 64 positions 73 -> 80).  256 single tokens of 32 heads 11.5 us, a million
+// sectors of 32 bytes written in part (with eight channels per thread 12.6).
+// Q = 4: four times as many threads, where a workgroup's 16 x 8 conversions are what a launch waits for: 16 tokens of 8 heads 7.5 -> 4.0
+// us, 24 x 64 tokens 8.8 -> 6.8, 512 of 40 heads 8.9 -> 6.7; 2 x 512 (340 workgroups of the other kind) 11.5 either way; and for rows that
+// fill a quarter of the other kind's: 100 x 300 tokens of 4 x 64 elements 22.5 -> 16.9, 32 prompts of 300 tokens, 40 heads 61 -> 88.
 template <typename S, int D, int Q, int N>
 __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqList<N> list) {
   typedef typename S::storage ST;
   typedef uint32_t words __attribute__((ext_vector_type(Q / 4)));
   constexpr int SL = kAppend8Slots, COLS = 64 * Q;     // elements of a token's row that a workgroup takes
+  __shared__ u32x4 turn[Q == 16 ? 2048 : 1];
   const int row = a.n_kv * D, u = blockIdx.x;
   const bool is_v = blockIdx.y & 1;
   int rec = -1;                                        // the last sequence whose first unit is not behind u
@@ -70,73 +74,109 @@ __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqLi
     return;
   }
   const int e0 = c0 + (threadIdx.x % (8 * Q)) * 8, h = threadIdx.x / (8 * Q);
-  if (e0 >= row || s1 <= Q * h || s0 >= Q * h + Q) return;
-  const int g = e0 / D;
-  const float scale = is_v ? a.v_scale[g] : a.k_scale[g], r = 1.f / scale;
-  const ST* const src = reinterpret_cast<const ST*>(is_v ? a.v_new : a.k_new) + t0 * row + e0;
-  uint8_t* const dst = base + (is_v ? (int64_t)row * a.pb + (int64_t)e0 * a.pb + slot0 : ((int64_t)g * a.pb + slot0) * D + (e0 - g * D));
-  const auto bytes8 = [&](u32x4 x) {
-    ST e[8];
-    __builtin_memcpy(e, &x, 16);
-    float f[8];
+  const bool turned = Q == 16 && is_v && s1 - s0 == SL;               // a whole run: by way of LDS, whole lines to memory
+  if (!turned && (e0 >= row || s1 <= Q * h || s0 >= Q * h + Q)) return;
+  if (e0 < row) {
+    const int g = e0 / D;
+    const float scale = is_v ? a.v_scale[g] : a.k_scale[g], r = 1.f / scale;
+    const ST* const src = reinterpret_cast<const ST*>(is_v ? a.v_new : a.k_new) + t0 * row + e0;
+    uint8_t* const dst = base + (is_v ? (int64_t)row * a.pb + (int64_t)e0 * a.pb + slot0 : ((int64_t)g * a.pb + slot0) * D + (e0 - g * D));
+    const auto bytes8 = [&](u32x4 x) {
+      ST e[8];
+      __builtin_memcpy(e, &x, 16);
+      float f[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = quotient(S::to_float(e[i]), scale, r);
-    uint2 w = make_uint2(0, 0);
-    w.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], w.x, false);
-    w.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w.x, true);
-    w.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[4], f[5], w.y, false);
-    w.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[6], f[7], w.y, true);
-    return w;
-  };
-  if (s1 - s0 <= 2) {                                  // K
-    for (int s = s0 > Q * h ? s0 : Q * h; s < s1 && s < Q * h + Q; ++s)
-      *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = bytes8(*reinterpret_cast<const u32x4*>(src + (int64_t)s * row));
-    return;
-  }
-  u32x4 x[Q];
-#pragma unroll
-  for (int i = 0; i < Q; ++i) {
-    const int s = Q * h + i;
-    if (s >= s0 && s < s1) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (int64_t)s * row));
-  }
-  uint2 by_slot[Q];
-#pragma unroll
-  for (int i = 0; i < Q; ++i) {
-    const int s = Q * h + i;
-    by_slot[i] = bytes8(x[i]);
-    if (!is_v && s >= s0 && s < s1) *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = by_slot[i];
-  }
-  if (!is_v) return;
-#pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    words* const at = reinterpret_cast<words*>(dst + (int64_t)c * a.pb + Q * h);
-    words w;
-#pragma unroll
-    for (int q = 0; q < Q / 4; ++q) {
-      uint32_t b = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) b |= (((c < 4 ? by_slot[4 * q + i].x : by_slot[4 * q + i].y) >> (8 * (c & 3))) & 0xffu) << (8 * i);
-      w[q] = b;
+      for (int i = 0; i < 8; ++i) f[i] = quotient(S::to_float(e[i]), scale, r);
+      uint2 w = make_uint2(0, 0);
+      w.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], w.x, false);
+      w.x = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w.x, true);
+      w.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[4], f[5], w.y, false);
+      w.y = __builtin_amdgcn_cvt_pk_fp8_f32(f[6], f[7], w.y, true);
+      return w;
+    };
+    if (s1 - s0 <= 2) {                                // K
+      for (int s = s0 > Q * h ? s0 : Q * h; s < s1 && s < Q * h + Q; ++s)
+        *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = bytes8(*reinterpret_cast<const u32x4*>(src + (int64_t)s * row));
+      return;
     }
-    if (s0 > Q * h || s1 < Q * h + Q) {
-      const words old = *at;
+    u32x4 x[Q];
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      const int s = Q * h + i;
+      if (s >= s0 && s < s1) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (int64_t)s * row));
+    }
+    uint2 by_slot[Q];
+#pragma unroll
+    for (int i = 0; i < Q; ++i) {
+      const int s = Q * h + i;
+      by_slot[i] = bytes8(x[i]);
+      if (!is_v && s >= s0 && s < s1) *reinterpret_cast<uint2*>(dst + (int64_t)s * D) = by_slot[i];
+    }
+    if (!is_v) return;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      words* const at = reinterpret_cast<words*>(dst + (int64_t)c * a.pb + Q * h);
+      words w;
 #pragma unroll
       for (int q = 0; q < Q / 4; ++q) {
-        uint32_t mask = 0;
+        uint32_t b = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mask |= Q * h + 4 * q + i >= s0 && Q * h + 4 * q + i < s1 ? 0xffu << (8 * i) : 0u;
-        w[q] = (w[q] & mask) | (old[q] & ~mask);
+        for (int i = 0; i < 4; ++i) b |= (((c < 4 ? by_slot[4 * q + i].x : by_slot[4 * q + i].y) >> (8 * (c & 3))) & 0xffu) << (8 * i);
+        w[q] = b;
       }
+      if constexpr (Q == 16) {
+        if (turned) {                                  // channel 8 i + c's half h in place 16 i + 2 c + h, the low four bits by i: no two lanes on a bank
+          const int i = threadIdx.x & 127;
+          turn[16 * i + ((2 * c + h) ^ (i & 15))] = w;
+          continue;
+        }
+      }
+      if (s0 > Q * h || s1 < Q * h + Q) {
+        const words old = *at;
+#pragma unroll
+        for (int q = 0; q < Q / 4; ++q) {
+          uint32_t mask = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mask |= Q * h + 4 * q + i >= s0 && Q * h + 4 * q + i < s1 ? 0xffu << (8 * i) : 0u;
+          w[q] = (w[q] & mask) | (old[q] & ~mask);
+        }
+      }
+      *at = w;
     }
-    *at = w;
+  }
+  if constexpr (Q == 16) {
+    if (!turned) return;
+    __syncthreads();
+    const bool stream = a.pb == SL &&                  // whole lines, and more bytes than the last cache holds
+                         (int64_t)gridDim.x * (2 * SL) * row > (int64_t)256 << 20;
+    const auto move = [&](auto past) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int at = 256 * j + threadIdx.x, ch = at >> 1;
+        if (c0 + ch >= row) break;
+        u32x4* const to = reinterpret_cast<u32x4*>(base + ((int64_t)row + c0 + ch) * a.pb + slot0 + 16 * (at & 1));
+        const u32x4 w = turn[(at & ~15) | ((at & 15) ^ ((at >> 4) & 15))];
+        if constexpr (decltype(past)::value)
+          __builtin_nontemporal_store(w, to);
+        else
+          *to = w;
+      }
+    };
+    if (stream) {
+      asm volatile("");                                // or the compiler makes one of the two
+      move(std::true_type());
+      asm volatile("");
+    } else {
+      move(std::false_type());
+    }
   }
 }
 
 // One workgroup per (sequence, kv head).  Bound by latency (one path of 16 tokens, 8 heads 4.7 us) and, in large batches, by the lines of V
-// that the paths' elements lie in, nearly all of the new tokens' blocks (128 paths, 40 heads 24 us): the path, its length and the blocks that the new tokens lie in are requested
-// together, then 32 places of the path at a time are read, K 16 bytes and V an element per access with neighbouring threads on
-// neighbouring places of a channel, and stored behind a barrier.  A place is never behind the token that comes to it, so what is
-// stored for these places is not read for later ones.
+// that the paths' elements lie in, nearly all of the new tokens' blocks (128 paths, 40 heads 24 us).  The path, its length and the blocks
+// that the new tokens lie in are requested together, then 32 places of the path at a time are read, K 16 bytes and V an element per
+// access with neighbouring threads on neighbouring places of a channel, and stored behind a barrier.  A place is never behind the
+// token that comes to it, so what is stored for these places is not read for later ones.
 template <int ES, int D, int N>
 __global__ __launch_bounds__(256) void kv_accept_kernel(FlpStepArgs a, FlpSeqList<N> list, const int32_t* __restrict__ n_accept,
                                                         const int32_t* __restrict__ path) {
@@ -225,7 +265,7 @@ flp_status flp_launch_kv_append8(int dtype, int head_dim, const FlpStepArgs& a, 
                                  hipStream_t stream) {
   if (n_units <= 0) return FLP_OK;
   const int row = a.n_kv * head_dim, wide = 2 * ((row + 1023) / 1024);
-  const bool few = (int64_t)n_units * wide < 256;      // less than a workgroup for every CU
+  const bool few = row <= 256 || (int64_t)n_units * wide < 256;      // fewer workgroups than CUs
   const dim3 grid((unsigned)n_units, few ? 2 * (unsigned)((row + 255) / 256) : (unsigned)wide);
   with_list(list, [&](const auto& l) {
     constexpr int N = sizeof(l.prefix) / sizeof(int32_t);

@@ -184,6 +184,28 @@ def test_append8_of_large_batches(heads, bt):
     assert same(s.now(), s.append_oracle())
 
 
+def test_append8_past_the_caches():
+    """More than the caches hold: the last prompt's K and V against the oracle, and the first one's."""
+    n, lens = 18, 2500
+    seqs = [(i % 3 * 11, lens) for i in range(n)]
+    s = Setup("f16", 50, 50, 64, [seqs[0], seqs[-1]], kv8=True, seed=36)
+    one = np.concatenate([s.k_new[:lens], s.k_new[:lens]]), np.concatenate([s.v_new[:lens], s.v_new[:lens]])
+    s.device()
+    nb = -(-(22 + lens) // 32)
+    image = torch.zeros((n * nb, s.image.shape[1]), dtype=torch.uint8, device="cuda")
+    pool = flpool.Pool("f16", 50, 64, n * nb, 0, dev=image)
+    tables = torch.arange(n * nb, dtype=torch.int32, device="cuda").view(n, nb)
+    cu, P = np.arange(n + 1, dtype=np.int32) * lens, np.array([p for p, _ in seqs], np.int32)
+    k, v = (up(x[:lens]).repeat(n, 1, 1) for x in one)
+    pool.kv_append8(k, v, s.t["ks"], s.t["vs"], cu, P, tables)
+    torch.cuda.synchronize()
+    for i in (0, 1, n - 1):
+        want = np.zeros((nb, s.image.shape[1]), np.uint8)
+        kk, vv = (so.quantise(wl.dequantize(x[:lens], "f16"), sc) for x, sc in zip(one, (s.ks, s.vs)))
+        so.store(want, np.arange(nb, dtype=np.int32), int(P[i]), kk, vv, 50, 64, 32)
+        assert same(image[i * nb:(i + 1) * nb].cpu().numpy(), want), i
+
+
 def test_append8_of_many_sequences_and_scales():
     """More sequences than travel in a launch's arguments; quotients of many scales, ties among them."""
     r = np.random.default_rng(5)
