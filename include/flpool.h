@@ -159,17 +159,19 @@ flp_status flp_paged_prefix_attention(flp_pool* pool, const flp_attn_batch* batc
  * These calls (and the tree and accept calls further down) allocate nothing and keep no state, but for attention calls whose batch
  * needs a staging slot (more than 224 sequences with new tokens) or the pool's workspace (contexts that are cut into pieces over
  * workgroups, as long ones of small batches are), and tree calls that append K and V of the pool's type: under stream capture
- * these are refused (FLP_ENOTSUP, nothing enqueued).  All others can be captured into a HIP graph and replayed.  Calls on
- * several streams owe each other no order but that of the data.  The pool's device must be the current one (FLP_EINVAL). */
+ * these are refused (FLP_ENOTSUP, nothing enqueued).  All others can be captured into a HIP graph and replayed, with the lengths
+ * that they were captured with.  Calls on several streams owe each other no order but that of the data.  `out` overlaps no input.  The
+ * pool's device must be the current one (FLP_EINVAL). */
 typedef struct {
-  const float* k_scale;           /* device float[n_kv_heads], finite and > 0                 */
-  const float* v_scale;           /* device float[n_kv_heads], finite and > 0                 */
+  const float* k_scale;           /* device float[n_kv_heads], 2^-100 to 2^100                */
+  const float* v_scale;           /* device float[n_kv_heads], 2^-100 to 2^100                */
 } flp_kv8_scales;
 
 int64_t flp_pool_kv8_block_tokens(const flp_pool* pool);   /* 0: the pool holds no 8-bit cache */
 
 /* Quantise the new tokens' K and V into their slots: the byte is x / scale in fp32, limited to [-448, 448] (infinities
- * too), rounded to e4m3 to nearest even; a NaN stays NaN.  Every other slot keeps what it holds.  Arguments as for flp_kv_append. */
+ * too), rounded to e4m3 to nearest even; a NaN stays NaN.  Every other slot keeps what it holds (slots of V beside the new ones
+ * are written again as they are: a block that gets new tokens belongs to one sequence).  Arguments as for flp_kv_append. */
 flp_status flp_kv_append8(flp_pool* pool, const flp_attn_batch* batch, const flp_kv8_scales* scales, void* hip_stream);
 
 /* flp_paged_prefix_attention over such a cache; with k_new and v_new flp_kv_append8 is enqueued first (the new tokens attend
