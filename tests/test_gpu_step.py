@@ -176,7 +176,7 @@ def test_append8(dtype, heads, bt):
 
 
 @pytest.mark.parametrize("bt", [16, 32])
-@pytest.mark.parametrize("heads", [(8, 2, 128), (40, 40, 128), (5, 5, 64)])
+@pytest.mark.parametrize("heads", [(8, 2, 128), (20, 20, 128), (5, 5, 64)])
 def test_append8_of_large_batches(heads, bt):
     """Launches with a workgroup for every CU: runs that are whole and cut, single slots, rows that end inside a workgroup's channels."""
     s = Setup("bf16", *heads, ENDS * 14 + [(5, 1)] * 40 + [(31, 2)] * 9, kv8=True, bt=bt, seed=35).device()
@@ -338,10 +338,9 @@ WAYS = [  # name, heads, sequences, the launches in 16 bits, and in 8
 ]
 
 
-@pytest.mark.parametrize("kind", ["f16", "bf16", "f16 8", "bf16 8"])
-@pytest.mark.parametrize("bt", [16, 32])
+@pytest.mark.parametrize("kind,bt", [("f16", 32), ("bf16", 16), ("f16 8", 16), ("bf16 8", 32)])
 @pytest.mark.parametrize("way", WAYS, ids=lambda w: w[0])
-def test_trees_every_way(way, bt, kind):
+def test_trees_every_way(way, kind, bt):
     """Trees by every launch that the plan knows, tokens without any bit and K and V that are not finite and hidden from some rows among them."""
     _, heads, seqs, in16, in8 = way
     dtype, kv8 = kind.split()[0], kind.endswith("8")
@@ -600,3 +599,83 @@ def test_two_streams_share_the_pieces_workspace():
     s.out = outs[0]
     s.check(lambda i: so.causal(*s.seqs[i]))
     assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+def test_replays_between_eager_calls():
+    """A captured step of more sequences than the short list holds, replayed between eager calls that cut contexts on the same pool."""
+    seqs = spread(40, 0, 300, [1, 4, 0, 9])
+    s = Setup("bf16", 8, 2, 128, seqs, kv8=True, seed=40).device()
+    r = np.random.default_rng(41)
+    masks = [random_tree(r, n) for _, n in seqs]
+    s.tree(masks, append=True)
+    torch.cuda.synchronize()
+    want_out, want_image, start = s.out.clone(), s.t["image"].clone(), up(s.image)
+    long = np.array([0, 2], np.int32), np.array([4000], np.int32)
+    blocks = torch.randint(0, s.n_blocks, (1, 200), dtype=torch.int32, device="cuda")
+    q, eager = s.t["q"][:2].contiguous(), torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda")
+    cut = lambda: s.pool.paged_prefix_attention8(q, eager, s.t["ks"], s.t["vs"], *long, blocks, n_q_heads=8)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        more = dict(k_new=s.t["k_new"], v_new=s.t["v_new"], k_scale=s.t["ks"], v_scale=s.t["vs"])
+        s.pool.paged_tree_attention(s.t["q"], s.out, s.mask, *s.where, n_q_heads=8, **more)
+    first = None
+    for i in range(5):
+        s.t["image"].copy_(start)
+        s.out.fill_(7)
+        g.replay()
+        cut()
+        torch.cuda.synchronize()
+        first = eager.clone() if first is None else first
+        assert torch.equal(s.t["image"], want_image) and torch.equal(s.out, want_out), i
+        assert same(eager.view(torch.int16).cpu().numpy(), first.view(torch.int16).cpu().numpy()), i
+
+
+def test_threads_share_a_pool():
+    """Two threads, each with a stream and calls of its own kind on one pool: cut contexts, staged lists and single launches."""
+    import threading
+    s = Setup("f16", 8, 2, 128, [(4000, 2), (3000, 3)] + spread(230, 0, 40, [1]), kv8=True, seed=42).device()
+    single = Setup("f16", 8, 2, 128, [(50, 1)], kv8=True, seed=43).device()
+    want = []
+    for x in (s, single):
+        x.prefix8()
+        x.check(lambda i: so.causal(*x.seqs[i]))
+        want.append(x.out.clone())
+    failures = []
+
+    def run(mine):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for i in range(60):
+                    x, w = ((s, want[0]), (single, want[1]))[(i + mine) % 3 == 0]
+                    out = torch.full_like(w, 3.0)
+                    out[x.T:] = 7
+                    x.pool.paged_prefix_attention8(x.t["q"], out, x.t["ks"], x.t["vs"], *x.where, n_q_heads=8, stream=stream)
+                    stream.synchronize()
+                    if not torch.equal(out, w):
+                        failures.append((mine, i))
+        except Exception as e:                             # a thread's own would be lost
+            failures.append(repr(e))
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures
+
+
+@pytest.mark.parametrize("kind", ["f16", "f16 8"])
+def test_sequences_that_share_blocks(kind):
+    """Drafts of several sequences over one shared prefix, and one sequence that is listed three times."""
+    s = Setup(kind.split()[0], 8, 2, 128, [(96, 7), (96, 12), (96, 1), (96, 7), (96, 7)], kv8=kind.endswith("8"), seed=44)
+    whole = 96 // s.pb
+    s.tables[:, :whole] = s.tables[0, :whole]
+    s.tables[3:] = s.tables[0]
+    r = np.random.default_rng(45)
+    masks = [random_tree(r, n) for _, n in s.seqs]
+    s.device()
+    s.tree(masks)
+    s.check(lambda i: so.tree(*s.seqs[i], masks[i]))
+    assert same(s.now(), s.image)
