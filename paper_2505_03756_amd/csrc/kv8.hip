@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256) void kv_append8_kernel(FlpStepArgs a, FlpSeqLi
         w[q] = b;
       }
       if constexpr (Q == 16) {
-        if (turned) {                                  // channel 8 i + c's half h in place 16 i + 2 c + h, the low four bits by i: no two lanes on a bank
+        if (turned) {                                  // channel 8 i + c's half h: place 16 i + 2 c + h, the low four bits turned by i for the banks
           const int i = threadIdx.x & 127;
           turn[16 * i + ((2 * c + h) ^ (i & 15))] = w;
           continue;

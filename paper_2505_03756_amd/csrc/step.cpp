@@ -1,5 +1,5 @@
 // Host side of the calls over an 8-bit cache, of drafted trees and of accepted paths: argument checks, the records of the
-// sequences, and the launches.  C ABI in flpool.h, kernels in attention_step.hip and kv8.hip.
+// sequences, and the launches.  C ABI in flpool.h, kernels in attention_step.hip, attention_step_tiles.hip and kv8.hip.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -114,7 +114,6 @@ FlpStepArgs make_args(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_
   a.scale_log2e = (b->sm_scale > 0.f ? b->sm_scale : 1.0f / std::sqrt((float)p->cfg.head_dim)) * 1.4426950408889634f;
   return a;
 }
-
 
 // Staging slots and the workspace are handed from call to call by events, which a replayed graph would not see
 flp_status refuse_capture(hipStream_t stream, const char* who) {
