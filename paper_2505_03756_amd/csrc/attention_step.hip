@@ -18,6 +18,9 @@
 //            is multiplied by zero first, and what is not finite goes another way (below).
 //   8 bit    e4m3 is exact in fp16 and in bf16: K is widened to the type of q, V and the weights to fp16, two pieces as well.
 //
+// Exponents are differences from the maximum before they are scaled: the product of a large maximum and the scale has more bits than a float,
+// and what its rounding leaves would be the exponent of the largest weight (scores of 2^34: infinite or all zero).
+//
 // A workgroup is four waves, eight in small launches.  Where the launch has enough of them they are independent, side by side on row tiles
 // of a (sequence, kv head), which then read the same K and V at about the same time, or on kv heads; otherwise they take slices of the
 // context, merged in LDS.  Contexts of the smallest launches are cut into pieces over workgroups as well, because one CU
@@ -321,13 +324,13 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
         for (int i = 0; i < 4; ++i) O[ct][i] *= alpha;
     }
     vvec w[STEPS][C::PIECES];
-    const float mc = m == -INFINITY ? 0.f : m * c;     // nothing seen yet: weights 0
+    const float base = m == -INFINITY ? 0.f : m;       // nothing seen yet: weights 0
     float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][i], c, -mc));
+        const float x = __builtin_amdgcn_exp2f((s[t][i] - base) * c);
         sum += x;
         const int e = 4 * t + i;
         put(w[e / VE][0], e % VE, x);

@@ -104,8 +104,12 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) qf[j][kk] = as_vec<vec>(*reinterpret_cast<const u32x4*>(qp + 32 * kk));
   }
-  f32x4 O[8][2];
+  // Scores are differences from the running maximum, as in attention_step.hip: its negative is what the first product adds to (subtracted
+  // from every score instead: the prompts below 229, the long trees 262 us)
+  const float lag = 8.f / c;
+  f32x4 O[8][2], base[2];
   float mrow[2] = {-INFINITY, -INFINITY}, lsum[2] = {0.f, 0.f};
+  base[0] = base[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
@@ -250,7 +254,7 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        S[2 * (q >> 2) + i][j] = M::mfma(kf[i], qf[j][q & 3], q & 3 ? S[2 * (q >> 2) + i][j] : f32x4{0.f, 0.f, 0.f, 0.f});
+        S[2 * (q >> 2) + i][j] = M::mfma(kf[i], qf[j][q & 3], q & 3 ? S[2 * (q >> 2) + i][j] : base[j]);
   };
   const auto mask = [&](int t) {
     if (BN * t + BN <= wave_all_see) return;
@@ -282,14 +286,22 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) tm[j] = fmaxf(tm[j], S[k4][j][i]);
     }
-    if (__builtin_amdgcn_ballot_w64((tm[0] - mrow[0]) * c > 8.f || (tm[1] - mrow[1]) * c > 8.f)) {
+    // a maximum of minus infinity: nothing seen yet
+    if (__builtin_amdgcn_ballot_w64(tm[0] > (mrow[0] == -INFINITY ? -INFINITY : lag) || tm[1] > (mrow[1] == -INFINITY ? -INFINITY : lag))) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         tm[j] = fmaxf(tm[j], __shfl_xor(tm[j], 16));
         tm[j] = fmaxf(tm[j], __shfl_xor(tm[j], 32));
-        const float m_new = fmaxf(mrow[j], tm[j]);
-        const float alpha = m_new == mrow[j] ? 1.f : __builtin_amdgcn_exp2f((mrow[j] - m_new) * c);
-        mrow[j] = m_new;
+        const bool first = mrow[j] == -INFINITY;
+        const float up = !first ? fmaxf(tm[j], 0.f) : tm[j] == -INFINITY ? 0.f : tm[j];
+        const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-up * c);
+        mrow[j] = first ? tm[j] : mrow[j] + up;
+        const float from = first && tm[j] == -INFINITY ? 0.f : -mrow[j];
+        base[j] = f32x4{from, from, from, from};
+#pragma unroll
+        for (int k4 = 0; k4 < 4; ++k4)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) S[k4][j][i] -= up;
         lsum[j] *= alpha;
 #pragma unroll
         for (int ct = 0; ct < 8; ++ct)
@@ -298,10 +310,10 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
       }
     }
   };
-  const auto weights = [&](int j, int b, float mc) {
+  const auto weights = [&](int j, int b) {
     float p[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(S[2 * b + (e >> 2)][j][e & 3], c, -mc));
+    for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(S[2 * b + (e >> 2)][j][e & 3] * c);
     Pw[j][b] = MV::pack(p, lsum[j]);
   };
   const auto step = [&](int kt) {
@@ -324,9 +336,8 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
     __builtin_amdgcn_sched_barrier(0);
     mask(kt);
     raise();
-    const float mc[2] = {mrow[0] == -INFINITY ? 0.f : mrow[0] * c, mrow[1] == -INFINITY ? 0.f : mrow[1] * c};      // nothing seen yet: weights 0
 #pragma unroll
-    for (int q = 0; q < 4; ++q) weights(q & 1, q >> 1, mc[q & 1]);
+    for (int q = 0; q < 4; ++q) weights(q & 1, q >> 1);
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
       if (q < 6) load_v(vf[(q + 2) % 3], buf, q + 2);
