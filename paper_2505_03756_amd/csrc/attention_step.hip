@@ -13,10 +13,16 @@
 // K are one step in 16 bits, two in 8, four (16x16x4) in fp32.
 //
 //   fp32     fp32 instructions throughout.
-//   16 bit   weights in two pieces of the pool's type, the value and its remainder: 16 bits of them in bf16 and 22 in fp16, where one
-//            piece would add an error as large as the rounding of the result.  An infinite V would meet a negative remainder, so V
-//            is multiplied by zero first, and what is not finite goes another way (below).
+//   16 bit   weights in two pieces of the pool's type, the value and its remainder, where one piece would add an error as large as the
+//            rounding of the result.  An infinite V would meet a negative remainder, so V is multiplied by zero first, and what is
+//            not finite goes another way (below).
 //   8 bit    e4m3 is exact in fp16 and in bf16: K is widened to the type of q, V and the weights to fp16, two pieces as well.
+//
+// In bf16 the pieces hold 16 bits of a weight whatever its size.  In fp16 they hold 22, but nothing below 2^-24, which a long context under one
+// dominant key is full of.  So the weight at the running maximum is 2^10 there (LIFT), and the maximum is raised when a row outgrows it
+// by 2^5 (LAG), so that no weight exceeds 2^15; a weight is off by 2^-22 of itself or 2^-35 of the largest, whichever is more.  The lift is the
+// weights' sum's as well.  More of it leaves less room above the maximum: 2^13 and 2^2 made the tiled kernel's long trees 271 us
+// instead of 253 (2^7 and 2^8: 251), for raising the maximum in so many steps.
 //
 // Exponents are differences from the maximum before they are scaled: the product of a large maximum and the scale has more bits than a float,
 // and what its rounding leaves would be the exponent of the largest weight (scores of 2^34: infinite or all zero).
@@ -206,6 +212,8 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
     }
   }
 
+  constexpr bool FP16_W = std::is_same<vvec, h16x8>::value;
+  constexpr float LIFT = FP16_W ? 10.f : 0.f, LAG = FP16_W ? 5.f : 8.f, UNLIFT = FP16_W ? 0x1p-10f : 1.f;
   f32x4 O[CT];
   float m = -INFINITY, l = 0.f;
 #pragma unroll
@@ -305,13 +313,13 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
       }
     }
 
-    // The running maximum is raised only when a row has outgrown it by 2^8: until then weights are relative to the old one
+    // The running maximum is raised only when a row has outgrown it by 2^LAG: until then weights are relative to the old one
     float tm = s[0][0];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) tm = fmaxf(tm, s[t][i]);
-    if (__builtin_amdgcn_ballot_w64((tm - m) * c > 8.f)) {
+    if (__builtin_amdgcn_ballot_w64((tm - m) * c > LAG)) {
       tm = fmaxf(tm, __shfl_xor(tm, 16));
       tm = fmaxf(tm, __shfl_xor(tm, 32));
       const float mn = fmaxf(m, tm);
@@ -330,7 +338,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = __builtin_amdgcn_exp2f((s[t][i] - base) * c);
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[t][i] - base, c, LIFT));
         sum += x;
         const int e = 4 * t + i;
         put(w[e / VE][0], e % VE, x);
@@ -411,10 +419,10 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
     total = fmaf(ml[x].y, factor[x], total);
   }
   const bool nothing = a.mask && P == 0 && bits == 0;
-  const float inv = vs / total;
+  const float inv = 1.f / total;                       // apart from the scale, which may be as small as 2^-100
   const int64_t prow = (int64_t)rec.part0 + (int64_t)tok * rec.pieces + piece;
   float* const pp = a.partials + (prow * a.n_h + (g * G + (rc - tok * G))) * (D + 2);
-  if (r < R && rec.pieces > 1 && lh == 0 && slice == 0 && ch0 == 0) *reinterpret_cast<float2*>(pp) = make_float2(M * c, total);
+  if (r < R && rec.pieces > 1 && lh == 0 && slice == 0 && ch0 == 0) *reinterpret_cast<float2*>(pp) = make_float2(M * c, total * UNLIFT);
 #pragma unroll 1
   for (int ct = slice; ct < CT; ct += kw) {
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -428,14 +436,15 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
     if (r >= R) continue;
     if (rec.pieces > 1) {
       float2* const d2 = reinterpret_cast<float2*>(pp + 2 + ch0 + 16 * ct + 4 * lh);
-      d2[0] = make_float2(o[0] * vs, o[1] * vs);
-      d2[1] = make_float2(o[2] * vs, o[3] * vs);
+      const float f = vs * UNLIFT;                     // or a scale of 2^100 would have no room for the sum
+      d2[0] = make_float2(o[0] * f, o[1] * f);
+      d2[1] = make_float2(o[2] * f, o[3] * f);
       continue;
     }
     ST* const op = reinterpret_cast<ST*>(a.out) + rowoff + ch0 + 16 * ct + 4 * lh;
     ST e[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) e[i] = S::from_float(nothing ? 0.f : o[i] * inv);
+    for (int i = 0; i < 4; ++i) e[i] = S::from_float(nothing ? 0.f : o[i] * inv * vs);
     __builtin_memcpy(__builtin_assume_aligned(op, 4 * sizeof(ST)), e, sizeof(e));
   }
 }

@@ -12,8 +12,9 @@
 //            position or by bit of the tree, and added at the end to the rows that see them.
 //   pieces   Contexts of small launches are cut over workgroups as in attention_step.hip and merged by its merge kernel.
 //
-// Weights are rounded to 16 bits once, and their sum is taken as rounded: the error this adds is that of rounding the result, which the few
-// rows of attention_step.hip, bound by memory, avoid with a second piece at no cost.
+// Weights are rounded to 16 bits once, and their sum is taken as rounded: an error of half a step of each weight, about as large as that of
+// rounding the result, which the few rows of attention_step.hip, bound by memory, avoid with a second piece at no cost.  fp16 weights are
+// lifted as there against the end of fp16's range: one is off by 2^-11 of itself or 2^-35 of the largest, whichever is more.
 //
 // Measured: 16 prompts of 128 to 512 tokens over prefixes of up to 2048, 40 heads, fp16 over 8 bits, 120 GFLOP 214 us; 8 trees of 32 to 64
 // tokens over 8 to 16 k positions, 64 / 8 heads, bf16 over 8 bits, 158 GFLOP 225 us and 19 for the merge; a step of a workgroup (256 rows, 64
@@ -104,9 +105,11 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) qf[j][kk] = as_vec<vec>(*reinterpret_cast<const u32x4*>(qp + 32 * kk));
   }
-  // Scores are differences from the running maximum, as in attention_step.hip: its negative is what the first product adds to (subtracted
+  constexpr bool FP16_W = std::is_same<MV, MF16>::value;
+  constexpr float LIFT = FP16_W ? 10.f : 0.f, LAG = FP16_W ? 5.f : 8.f, UNLIFT = FP16_W ? 0x1p-10f : 1.f;      // as in attention_step.hip
+  // Scores are differences from the running maximum, as there: its negative is what the first product adds to (subtracted
   // from every score instead: the prompts below 229, the long trees 262 us)
-  const float lag = 8.f / c;
+  const float lag = LAG / c;
   f32x4 O[8][2], base[2];
   float mrow[2] = {-INFINITY, -INFINITY}, lsum[2] = {0.f, 0.f};
   base[0] = base[1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -276,7 +279,7 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
         for (int e = 0; e < 8; ++e) S[2 * b + (e >> 2)][j][e & 3] = (vis >> e) & 1 ? S[2 * b + (e >> 2)][j][e & 3] : -INFINITY;
       }
   };
-  const auto raise = [&]() {                                         // only where a row has outgrown its maximum by 2^8
+  const auto raise = [&]() {                                         // only where a row has outgrown its maximum by 2^LAG
     float tm[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -313,7 +316,7 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
   const auto weights = [&](int j, int b) {
     float p[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(S[2 * b + (e >> 2)][j][e & 3] * c);
+    for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(S[2 * b + (e >> 2)][j][e & 3], c, LIFT));
     Pw[j][b] = MV::pack(p, lsum[j]);
   };
   const auto step = [&](int kt) {
@@ -436,23 +439,23 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
     if (rec.pieces > 1) {
       const int64_t head = rowoff[j] / D - (rec.t0 + tok) * a.n_h;
       float* const pp = a.partials + ((rec.part0 + tok * rec.pieces + piece) * a.n_h + head) * (D + 2);
-      if (lh == 0) *reinterpret_cast<float2*>(pp) = make_float2(mrow[j] * c, l);
+      if (lh == 0) *reinterpret_cast<float2*>(pp) = make_float2(mrow[j] * c, l * UNLIFT);
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) {
         float2* const d2 = reinterpret_cast<float2*>(pp + 2 + 16 * ct + 4 * lh);
-        d2[0] = make_float2(O[ct][j][0] * vs, O[ct][j][1] * vs);
-        d2[1] = make_float2(O[ct][j][2] * vs, O[ct][j][3] * vs);
+        d2[0] = make_float2(O[ct][j][0] * (vs * UNLIFT), O[ct][j][1] * (vs * UNLIFT));
+        d2[1] = make_float2(O[ct][j][2] * (vs * UNLIFT), O[ct][j][3] * (vs * UNLIFT));
       }
       continue;
     }
     const bool nothing = tree && P == 0 && bits[j] == 0;
-    const float inv = vs / l;
+    const float inv = 1.f / l;
     uint16_t* op = reinterpret_cast<uint16_t*>(a.out) + rowoff[j] + 4 * lh;
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) {
       uint16_t o4[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o4[i] = nothing ? 0 : M::out(O[ct][j][i] * inv);
+      for (int i = 0; i < 4; ++i) o4[i] = nothing ? 0 : M::out(O[ct][j][i] * inv * vs);
       uint2 w;
       __builtin_memcpy(&w, o4, 8);
       *reinterpret_cast<uint2*>(op + 16 * ct) = w;
