@@ -185,7 +185,8 @@ flp_status flp_paged_prefix_attention8(flp_pool* pool, const flp_attn_batch* bat
  * New token j sees every position of the prefix and those new tokens j' of its sequence whose bit j' is set in
  * tree_mask[cu_new[i] + j]: its ancestors and, as a rule, itself.  Bits at or past the number of new tokens are ignored; a token that sees
  * nothing (no prefix, no bit) gets zeros.  What K and V of positions that a token does not see hold, infinities and NaN
- * included, does not reach its row.  Otherwise as flp_paged_prefix_attention (scales == NULL: the cache has the pool's type)
+ * included, does not reach its row; an infinity in V of a position that it sees is its channel's result however small the weight, a NaN or
+ * infinities of both signs make it NaN.  Otherwise as flp_paged_prefix_attention (scales == NULL: the cache has the pool's type)
  * or flp_paged_prefix_attention8.  tree_mask: device uint64[T], 8-byte aligned. */
 flp_status flp_paged_tree_attention(flp_pool* pool, const flp_attn_batch* batch, const uint64_t* tree_mask,
                                     const flp_kv8_scales* scales, void* hip_stream);

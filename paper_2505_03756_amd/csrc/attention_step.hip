@@ -39,7 +39,8 @@
 //
 // Infinities and NaN in V reach the rows that see them and no others: in the tiles where some row does not see everything, and in
 // all tiles of 16-bit V, values that are not finite are replaced by zero, and whether a row sees one is counted with products of
-// indicators.  Slots past the end of a sequence hold arbitrary bits and are replaced, never multiplied.
+// indicators.  They are put in where the slices have been added up: an infinity is the result's however small its weight, which may have
+// become zero on the way.  Slots past the end of a sequence hold arbitrary bits and are replaced, never multiplied.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -131,7 +132,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
   constexpr uint32_t ALL = (1u << RUN) - 1;
   __shared__ f32x4 merge_o[W][CT][64];
   __shared__ float2 merge_ml[W][16];
-  __shared__ uint8_t flags[W][CT][64];
+  __shared__ uint8_t flags[W][CT][64], any_flags[W];
 
   const int lane = threadIdx.x & 63, lr = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -390,27 +391,18 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
   if (lh == 0) merge_ml[wave][lr] = make_float2(m, l);
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) merge_o[wave][ct][lane] = O[ct];
-  if (__builtin_expect(flagged, 0))
-#pragma unroll 1
-    for (int ct = 0; ct < CT; ++ct) {
-      const uint32_t f = flags[wave][ct][lane];
-      f32x4 o = merge_o[wave][ct][lane];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if ((f >> i) & 1) o[i] += INFINITY;
-        if ((f >> (4 + i)) & 1) o[i] -= INFINITY;
-      }
-      merge_o[wave][ct][lane] = o;
-    }
+  if (lane == 0) any_flags[wave] = flagged;
   __syncthreads();
   if (!active) return;
   const int first = wave - slice * rw;
   float M = -INFINITY, total = 0.f, factor[W];
+  bool any = false;
   float2 ml[W];
 #pragma unroll
   for (int x = 0; x < W; ++x) {
     ml[x] = merge_ml[(first + x * rw) & (W - 1)][lr];
     if (x >= kw) ml[x] = make_float2(-INFINITY, 0.f);
+    else any = any || any_flags[(first + x * rw) & (W - 1)];
     M = fmaxf(M, ml[x].x);
   }
 #pragma unroll
@@ -432,6 +424,18 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
       if (x < kw)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], factor[x], o[i]);
+    }
+    if (__builtin_expect(any, 0)) {
+      uint32_t f = 0;
+      for (int x = 0; x < kw; ++x) {
+        const int y = (first + x * rw) & (W - 1);
+        if (any_flags[y]) f |= flags[y][ct][lane];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if ((f >> i) & 1) o[i] += INFINITY;
+        if ((f >> (4 + i)) & 1) o[i] -= INFINITY;
+      }
     }
     if (r >= R) continue;
     if (rec.pieces > 1) {
@@ -475,8 +479,9 @@ __global__ __launch_bounds__(256) void attn_step_merge_kernel(FlpStepArgs a, Lis
   float M = lane < ns ? mi : -INFINITY;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
-  // a piece that the row sees nothing of has m = -inf, l = 0 and zeros
-  const float wi = lane < ns && mi != -INFINITY ? (mi == M ? 1.f : exp2f(mi - M)) : 0.f;
+  // a piece that the row sees nothing of has m = -inf, l = 0 and zeros; any other a weight, 2^-149 (which is as near as its rounding) rather
+  // than zero, for the sake of its infinities
+  const float wi = lane < ns && mi != -INFINITY ? (mi == M ? 1.f : fmaxf(exp2f(mi - M), 0x1p-149f)) : 0.f;
   float l = lane < ns ? li * wi : 0.f;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) l += __shfl_xor(l, off);

@@ -9,7 +9,9 @@
 //            (K to the type of q, V to fp16, both exact), once for the eight waves.  Two stages, one barrier per tile.
 //   masks    A tile in which some row does not see every position is masked by what each row sees: positions up to its own, or its tree's bits.
 //            There, values of V that are not finite are taken out (8 bit: on their way to LDS; 16 bit: in LDS) and noted per channel, by
-//            position or by bit of the tree, and added at the end to the rows that see them.
+//            position or by bit of the tree, and put into the rows that see them at the end.  16-bit V of the prefix stays as it is in the
+//            products; where a result is not finite, the prefix is searched for the channels' infinities, which are the result's however
+//            small their weights (in the products a weight rounded to zero would make them NaN).
 //   pieces   Contexts of small launches are cut over workgroups as in attention_step.hip and merged by its merge kernel.
 //
 // Weights are rounded to 16 bits once, and their sum is taken as rounded: an error of half a step of each weight, about as large as that of
@@ -62,7 +64,8 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
   __shared__ __attribute__((aligned(16))) uint8_t smem[kStages * kStage];
   __shared__ int32_t tab_lds[kMfmaMaxBlocks];                        // the piece's part of the block table
   __shared__ uint64_t odd[2][D];                                     // V not finite: tree bits by sign (NaN both); causal: first NaN's position
-  __shared__ int32_t any_odd;
+  __shared__ uint32_t prefix_odd[KV8 ? 1 : D];                       // V of the prefix, as far as the piece has it: an infinity 1, its negative 2, NaN 3
+  __shared__ int32_t any_odd, broken;
 
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -130,8 +133,9 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
   if (tid < D) {
     odd[0][tid] = tree ? 0 : ~0ull >> 1;
     odd[1][tid] = 0;
+    if (!KV8) prefix_odd[tid] = 0;
   }
-  if (tid == 0) any_odd = 0;
+  if (tid == 0) any_odd = broken = 0;
   const auto clamped = [&](int grp) { return grp < last_grp ? grp : last_grp; };
   const auto block_of = [&](int grp) { return tab_lds[(clamped(grp) * BT >> psh) - blk_lo]; };
 
@@ -406,24 +410,56 @@ __global__ __launch_bounds__(512, 2) void attn_step_tiles_kernel(FlpStepArgs a, 
     enter(kt);
     request(kt);
   }
+  if constexpr (!KV8) {
+    float x = 0.f;                                                   // NaN where one of the sums is not finite
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x = fmaf(O[ct][j][i], 0.f, x);
+    if (__builtin_amdgcn_ballot_w64(x != x)) broken = 1;
+  }
   __builtin_amdgcn_s_waitcnt(kWaitVm0);                              // the look-ahead loads must land before the LDS is released
   __syncthreads();                                                   // and everybody's notes be there
+  if constexpr (!KV8) {
+    if (broken) {                                                    // a thread: a channel, every fourth run of 8 positions
+      constexpr uint16_t kInf = std::is_same<M, MF16>::value ? 0x7c00 : 0x7f80;
+      const int ch = tid & (D - 1), end = all_see < hi * BN ? all_see : hi * BN;
+      uint32_t found = 0;
+      for (int pos = lo * BN + 8 * (tid >> 7); pos < end; pos += 32) {
+        const uint8_t* const blk = a.pool + (int64_t)tab_lds[(pos >> psh) - blk_lo] * a.block_bytes + v_region;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(blk + (ch * pb + (pos & (pb - 1))) * 2);
+        uint16_t e[8];
+        __builtin_memcpy(e, &v, 16);
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+          const uint16_t size = e[s] & 0x7fff;
+          if (pos + s < end && size >= kInf) found |= size > kInf ? 3 : e[s] & 0x8000 ? 2 : 1;
+        }
+      }
+      if (found) atomicOr(&prefix_odd[ch], found);
+      __syncthreads();
+    }
+  }
 
   // ---- lane (row lr of tile j, quarter lh) holds channels 16 ct + 4 lh + (0..3)
   if (!wave_active) return;
-  if (any_odd) {
+  if (any_odd || (!KV8 && broken)) {
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint64_t up = odd[0][16 * ct + 4 * lh + i], down = odd[1][16 * ct + 4 * lh + i];
+        const int ch = 16 * ct + 4 * lh + i;
+        const uint64_t up = odd[0][ch], down = odd[1][ch];
+        const uint32_t before = KV8 ? 0 : prefix_odd[KV8 ? 0 : ch];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          if (tree) {
-            if (bits[j] & up) O[ct][j][i] += KV8 ? NAN : INFINITY;
-            if (bits[j] & down) O[ct][j][i] -= INFINITY;
-          } else if ((uint64_t)prow[j] >= up) {
-            O[ct][j][i] = NAN;
+          if (KV8) {                                                 // NaN alone
+            if (tree ? (bits[j] & up) != 0 : (uint64_t)prow[j] >= up) O[ct][j][i] = NAN;
+          } else {
+            const bool plus = (bits[j] & up) || (before & 1), minus = (bits[j] & down) || (before & 2);
+            if (plus || minus) O[ct][j][i] = plus && minus ? NAN : plus ? INFINITY : -INFINITY;
           }
         }
       }
