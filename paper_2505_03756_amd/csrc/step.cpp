@@ -336,8 +336,7 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
   a.mask = mask;
   const bool append16 = with_append && !sc;            // the pool's own append, whose units are staged
   if (staged || part_rows || append16) FLP_TRY(refuse_capture(stream, who));
-  if (append16) FLP_TRY(flp_enqueue_append(p, b, stream));
-  if (staged || part_rows) {
+  if (staged || part_rows) {                           // what may find no memory, before anything is enqueued
     if (part_rows) {
       void* w = nullptr;
       FLP_TRY(flp_attn_workspace(p, part_rows * b->n_q_heads * (p->cfg.head_dim + 2) * sizeof(float), stream, &w));
@@ -348,6 +347,7 @@ flp_status attend(flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc
     for (const AttnLaunch& l : launches)
       if (!inline_records(l)) to = std::copy(l.recs.begin(), l.recs.end(), to);
   }
+  if (append16) FLP_TRY(flp_enqueue_append(p, b, stream));
   flp_status s = staged ? flp_stage_upload(slot, staged * sizeof(FlpStepSeq), stream) : FLP_OK;
   if (s == FLP_OK && with_append && sc) s = append8(p, b, sc, stream);
   const FlpStepSeq* at = slot ? (const FlpStepSeq*)slot->dev : nullptr;
