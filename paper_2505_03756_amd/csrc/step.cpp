@@ -31,6 +31,14 @@ struct Call {
   int32_t most_new;            // new tokens that a sequence may have; 0: any number
 };
 
+flp_status check_heads(const flp_pool* p, const flp_attn_batch* b, const char* who) {
+  if (b->n_q_heads <= 0 || b->n_q_heads % p->cfg.n_kv_heads) {
+    flp_set_error("%s: n_q_heads %d is not a multiple of n_kv_heads %d", who, b->n_q_heads, p->cfg.n_kv_heads);
+    return FLP_EINVAL;
+  }
+  return FLP_OK;
+}
+
 // The checks of a batch; `recs`: the sequences with new tokens, unit0 and what follows still to be filled in
 flp_status check_batch(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, const Call& c, std::vector<FlpStepSeq>* recs) {
   if (!p || !b) {
@@ -55,10 +63,7 @@ flp_status check_batch(const flp_pool* p, const flp_attn_batch* b, const flp_kv8
     flp_set_error("%s: null or misaligned scales", c.who);
     return FLP_EINVAL;
   }
-  if (c.need_qo && (b->n_q_heads <= 0 || b->n_q_heads % p->cfg.n_kv_heads)) {
-    flp_set_error("%s: n_q_heads %d is not a multiple of n_kv_heads %d", c.who, b->n_q_heads, p->cfg.n_kv_heads);
-    return FLP_EINVAL;
-  }
+  if (c.need_qo) FLP_TRY(check_heads(p, b, c.who));
   if (b->n_seqs > 0 && b->cu_new[0] != 0) {
     flp_set_error("%s: cu_new[0] must be 0", c.who);
     return FLP_EINVAL;
@@ -390,16 +395,21 @@ flp_status guarded(const char* who, F f) {
 }  // namespace
 
 extern "C" int32_t flp_step_attention_route(const flp_pool* p, const flp_attn_batch* b, int32_t kv8) {
-  std::vector<FlpStepSeq> recs;
-  if (check_batch(p, b, nullptr, Call{"flp_step_attention_route", kv8 != 0, false, false, 0}, &recs) != FLP_OK) return -1;
-  size_t part_rows = 0;
+  static const char who[] = "flp_step_attention_route";
   int32_t route = 0;
-  for (const AttnLaunch& l : attn_plan(p, b->n_q_heads / p->cfg.n_kv_heads, kv8 ? 1 : p->elem_bytes, recs, &part_rows)) {
-    const int place = !inline_records(l) ? 3 : l.recs.size() <= (size_t)kShortList ? 0 : l.merge_rows ? 1 : 2;
-    const int split = l.tiles ? 0 : l.head_waves > 1 ? 1 : l.row_waves > 1 ? 2 : l.waves == 8 ? 3 : 0;
-    route |= (1 | (l.merge_rows ? 2 : 0) | 4 * place | 16 * split) << (l.tiles ? 8 : 0);
-  }
-  return route;
+  const flp_status s = guarded(who, [&]() -> flp_status {
+    std::vector<FlpStepSeq> recs;
+    FLP_TRY(check_batch(p, b, nullptr, Call{who, kv8 != 0, false, false, 0}, &recs));
+    FLP_TRY(check_heads(p, b, who));
+    size_t part_rows = 0;
+    for (const AttnLaunch& l : attn_plan(p, b->n_q_heads / p->cfg.n_kv_heads, kv8 ? 1 : p->elem_bytes, recs, &part_rows)) {
+      const int place = !inline_records(l) ? 3 : l.recs.size() <= (size_t)kShortList ? 0 : l.merge_rows ? 1 : 2;
+      const int split = l.tiles ? 0 : l.head_waves > 1 ? 1 : l.row_waves > 1 ? 2 : l.waves == 8 ? 3 : 0;
+      route |= (1 | (l.merge_rows ? 2 : 0) | 4 * place | 16 * split) << (l.tiles ? 8 : 0);
+    }
+    return FLP_OK;
+  });
+  return s == FLP_OK ? route : -1;
 }
 
 extern "C" int64_t flp_pool_kv8_block_tokens(const flp_pool* p) { return p ? kv8_tokens(p) : 0; }
