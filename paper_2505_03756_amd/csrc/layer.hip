@@ -466,7 +466,7 @@ extern "C" flp_status fll_qk_norm_rope(int32_t dtype, const void* q_in, int64_t 
     constexpr int U = decltype(unroll)::value;
     a.chunks = (groups + U - 1) / U;
     const int64_t blocks = ((int64_t)n_tokens * a.chunks + 3) / 4;
-    if (blocks > INT32_MAX) {
+    if (4 * blocks > kMaxWaves) {
       flp_set_error("fll_qk_norm_rope: more heads than one launch takes");
       return FLP_ERANGE;
     }

@@ -148,11 +148,23 @@ int64_t seq_list(const flp_attn_batch* b, int32_t first, FlpSeqList<kListSeqs>* 
   return units;
 }
 
+// before anything of the call is enqueued: every launch of its append takes its units, four waves each
+flp_status check_append8(const flp_attn_batch* b, const char* who) {
+  if (b->cu_new[b->n_seqs] / kAppend8Slots + 2 * kListSeqs <= kMaxWaves / 4) return FLP_OK;
+  FlpSeqList<kListSeqs> list;
+  for (int32_t first = 0; first < b->n_seqs; first += kListSeqs)
+    if (4 * seq_list(b, first, &list) > kMaxWaves) {
+      flp_set_error("%s: more new tokens than one launch takes", who);
+      return FLP_ERANGE;
+    }
+  return FLP_OK;
+}
+
 flp_status append8(const flp_pool* p, const flp_attn_batch* b, const flp_kv8_scales* sc, hipStream_t stream) {
   const FlpStepArgs a = make_args(p, b, sc, true);
   FlpSeqList<kListSeqs> list;
   for (int32_t first = 0; first < b->n_seqs; first += kListSeqs) {
-    const int64_t units = seq_list(b, first, &list);   // below 2^31: so are the new tokens
+    const int64_t units = seq_list(b, first, &list);
     FLP_TRY(flp_launch_kv_append8(p->cfg.dtype, p->cfg.head_dim, a, list, (int32_t)units, stream));
   }
   return FLP_OK;
@@ -173,7 +185,6 @@ bool inline_records(const AttnLaunch& l) {
 }
 
 constexpr int kMaxPieces = 64;
-constexpr int64_t kMaxWaves = (1ll << 26) - 1;         // of a launch: the runtime counts its threads in 32 bits
 constexpr int kWaveSlots = 512, kTileSlots = 256;      // workgroups of four waves, and of the tiled kernel, that the chip holds at once
 
 // The pieces of a launch's contexts, `piece` tiles at most, and the places that follow from them; tiles, groups: of each record, tiles
@@ -424,6 +435,7 @@ extern "C" flp_status flp_kv_append8(flp_pool* p, const flp_attn_batch* b, const
     }
     FLP_TRY(check_batch(p, b, sc, Call{who, true, false, true, 0}, &recs));
     if (recs.empty()) return FLP_OK;
+    FLP_TRY(check_append8(b, who));
     FLP_TRY(check_device(p, who));
     return append8(p, b, sc, (hipStream_t)hip_stream);
   });
@@ -440,6 +452,7 @@ extern "C" flp_status flp_paged_prefix_attention8(flp_pool* p, const flp_attn_ba
     const bool append = b && (b->k_new || b->v_new);
     FLP_TRY(check_batch(p, b, sc, Call{who, true, true, append, 0}, &recs));
     if (recs.empty()) return FLP_OK;
+    if (append) FLP_TRY(check_append8(b, who));
     FLP_TRY(check_device(p, who));
     return attend(p, b, sc, nullptr, append, recs, (hipStream_t)hip_stream, who);
   });
