@@ -283,17 +283,22 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkRows a, TurnTable t
     for (int o = 1; o < LPH; o <<= 1) ss += __shfl_xor(ss, o, 64);
     const float inv = 1.0f / sqrtf(ss / (float)D + a.eps);
     const bool is_q = h < a.n_q;
-    Vec<S> oa, ob;
+    float ra[N], rb[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const float af = S::to_float(x[u][0].e[j]) * inv * S::to_float(is_q ? w[0][0].e[j] : w[1][0].e[j]);
       const float bf = S::to_float(x[u][1].e[j]) * inv * S::to_float(is_q ? w[0][1].e[j] : w[1][1].e[j]);
-      // Which product is rounded, and that the sum is rounded before its conversion (fp16 has an instruction for both), is not left to the
-      // compiler, which decides for each u anew: a head's bits are the same wherever it comes among the heads of a call
-      float ra = fmaf(af, cv[j], -(bf * sv[j])), rb = fmaf(bf, cv[j], af * sv[j]);
-      asm("" : "+v"(ra), "+v"(rb));
-      oa.e[j] = S::from_float(ra);
-      ob.e[j] = S::from_float(rb);
+      ra[j] = fmaf(af, cv[j], -(bf * sv[j]));
+      rb[j] = fmaf(bf, cv[j], af * sv[j]);
+    }
+    // Which product is rounded, and that the sum is rounded before its conversion (fp16 has an instruction for both), is not left to the
+    // compiler, which decides for each u anew: a head's bits are the same wherever it comes among the heads of a call
+    Vec<S> oa, ob;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (std::is_same<S, F16>::value) asm("" : "+v"(ra[j]), "+v"(rb[j]));
+      oa.e[j] = S::from_float(ra[j]);
+      ob.e[j] = S::from_float(rb[j]);
     }
     ST* o = is_q ? (ST*)a.q_out + ((int64_t)t * a.n_q + h) * D : (ST*)a.k_out + ((int64_t)t * a.n_kv + (h - a.n_q)) * D;
     if (U > 1) {
