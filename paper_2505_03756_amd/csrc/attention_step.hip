@@ -132,7 +132,8 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
   constexpr uint32_t ALL = (1u << RUN) - 1;
   __shared__ f32x4 merge_o[W][CT][64];
   __shared__ float2 merge_ml[W][16];
-  __shared__ uint8_t flags[W][CT][64], any_flags[W];
+  __shared__ uint8_t flags[W][CT][64];
+  __shared__ __attribute__((aligned(8))) uint8_t any_flags[8];
 
   const int lane = threadIdx.x & 63, lr = lane & 15, lh = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -392,17 +393,17 @@ __global__ __launch_bounds__(64 * W, 2) void attn_step_kernel(FlpStepArgs a, Lis
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) merge_o[wave][ct][lane] = O[ct];
   if (lane == 0) any_flags[wave] = flagged;
+  if (W < 8 && lane == 1) any_flags[W + wave] = 0;
   __syncthreads();
   if (!active) return;
   const int first = wave - slice * rw;
   float M = -INFINITY, total = 0.f, factor[W];
-  bool any = false;
+  const bool any = *reinterpret_cast<const uint64_t*>(any_flags) != 0;
   float2 ml[W];
 #pragma unroll
   for (int x = 0; x < W; ++x) {
     ml[x] = merge_ml[(first + x * rw) & (W - 1)][lr];
     if (x >= kw) ml[x] = make_float2(-INFINITY, 0.f);
-    else any = any || any_flags[(first + x * rw) & (W - 1)];
     M = fmaxf(M, ml[x].x);
   }
 #pragma unroll
