@@ -128,7 +128,8 @@ typedef struct {
   const float*    v_scale;    /*   attention); both or neither                                                          */
 } fll_layer_options;
 
-/* fll_layer_forward with options (NULL: none). */
+/* fll_layer_forward with options (NULL: none).  What the attention refuses (flpool.h) is refused when the layer comes to it: h and the
+ * blocks are as they were then, scratch is not. */
 flp_status fll_layer_forward_options(flp_pool* pool, const fll_layer_config* cfg, const fll_layer_weights* w,
                                      const fll_layer_batch* batch, const fll_layer_options* options, void* h, void* scratch,
                                      int64_t scratch_bytes, void* hip_stream);

@@ -161,7 +161,9 @@ flp_status flp_paged_prefix_attention(flp_pool* pool, const flp_attn_batch* batc
  * workgroups, as long ones of small batches are), and tree calls that append K and V of the pool's type: under stream capture
  * these are refused (FLP_ENOTSUP, nothing enqueued).  All others can be captured into a HIP graph and replayed, with the lengths
  * that they were captured with.  Calls on several streams owe each other no order but that of the data.  `out` overlaps no input.  The
- * pool's device must be the current one (FLP_EINVAL). */
+ * pool's device must be the current one (FLP_EINVAL).  In 16-bit pools softmax weights are rounded to 16 bits once for sequences
+ * with many query rows and held in two such pieces for others; which is which goes by the whole batch, so in another one a sequence's
+ * result may differ by that rounding. */
 typedef struct {
   const float* k_scale;           /* device float[n_kv_heads], 2^-100 to 2^100                */
   const float* v_scale;           /* device float[n_kv_heads], 2^-100 to 2^100                */

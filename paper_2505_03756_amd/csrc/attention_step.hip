@@ -33,9 +33,9 @@
 // fetches no more than 64 bytes a nanosecond; a second launch merges them in piece order.  For the same reason launches of up to
 // half a workgroup per CU whose contexts are whole give each workgroup a part of V's channels and all of K (launch_kind).
 //
-// Bound by memory: 128 single tokens over 512 to 4096 positions, 32 heads, 8 bits, 2.48 GB: 420 us, 5.9 TB/s; small calls by the trips to
+// Bound by memory: 128 single tokens over 512 to 4096 positions, 32 heads, 8 bits, 2.48 GB: 424 us, 5.8 TB/s; small calls by the trips to
 // memory one after the other (arguments, block table, K and V) and by what a CU fetches: one token over 300 positions of 32 heads,
-// 8 bits, 7.3 us; a tree of 16 tokens over 700, 64 / 8 heads, bf16, 12.1 us.
+// 8 bits, 7.6 us; a tree of 16 tokens over 700, 64 / 8 heads, bf16, 12.4 us.
 //
 // Infinities and NaN in V reach the rows that see them and no others: in the tiles where some row does not see everything, and in
 // all tiles of 16-bit V, values that are not finite are replaced by zero, and whether a row sees one is counted with products of

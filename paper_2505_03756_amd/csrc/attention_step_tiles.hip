@@ -15,13 +15,14 @@
 //   pieces   Contexts of small launches are cut over workgroups as in attention_step.hip and merged by its merge kernel.
 //
 // Weights are rounded to 16 bits once, and their sum is taken as rounded: an error of half a step of each weight, about as large as that of
-// rounding the result, which the few rows of attention_step.hip, bound by memory, avoid with a second piece at no cost.  fp16 weights are
-// lifted as there against the end of fp16's range: one is off by 2^-11 of itself or 2^-35 of the largest, whichever is more.
+// rounding the result, which the few rows of attention_step.hip, bound by memory, avoid with a second piece at no cost (here it would cost
+// prompts 222 -> 277 us, long trees over 8 bits 253 -> 345, trees over fp16 277 -> 293).  fp16 weights are lifted as there against the end
+// of fp16's range: one is off by 2^-11 of itself or 2^-35 of the largest, whichever is more.
 //
-// Measured: 16 prompts of 128 to 512 tokens over prefixes of up to 2048, 40 heads, fp16 over 8 bits, 120 GFLOP 214 us; 8 trees of 32 to 64
-// tokens over 8 to 16 k positions, 64 / 8 heads, bf16 over 8 bits, 158 GFLOP 225 us and 19 for the merge; a step of a workgroup (256 rows, 64
+// Measured: 16 prompts of 128 to 512 tokens over prefixes of up to 2048, 40 heads, fp16 over 8 bits, 120 GFLOP 217 us; 8 trees of 32 to 64
+// tokens over 8 to 16 k positions, 64 / 8 heads, bf16 over 8 bits, 158 GFLOP 233 us and 18 for the merge; a step of a workgroup (256 rows, 64
 // positions) takes 1.8 us, of which the matrix instructions are 0.9: their issue and the vector work between the products bound it.  32
-// trees of 8 to 64 tokens over 256 to 4096 positions, 40 heads, fp16, 1.47 GB: 270 us, 5.4 TB/s.
+// trees of 8 to 64 tokens over 256 to 4096 positions, 40 heads, fp16, 1.47 GB: 276 us, 5.3 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
