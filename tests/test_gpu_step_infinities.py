@@ -22,8 +22,7 @@ WAYS = [  # name, heads, sequences, launches
 
 
 @pytest.mark.parametrize("below", [0.0, 45.0, 115.0])
-@pytest.mark.parametrize("bt", [16, 32])
-@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("kind,bt", [("f32", 16), ("f16", 32), ("bf16", 16)])
 @pytest.mark.parametrize("way", WAYS, ids=lambda w: w[0])
 def test_infinities_of_any_weight(way, kind, bt, below):
     """The first half of every prefix scores `below` under the rest: 45, a weight that 16 bits do not hold; 115, one that 32 do not."""

@@ -81,7 +81,7 @@ def check(s, sees, once, only=None):
     return worst_of
 
 
-@pytest.mark.parametrize("gap,wide", [(12.0, 0.0), (14.1, 0.0), (17.0, 1.5), (22.0, 0.0)])
+@pytest.mark.parametrize("gap,wide", [(14.1, 0.0), (17.0, 1.5), (22.0, 0.0)])
 @pytest.mark.parametrize("kind", ["f16", "bf16", "f16 8", "bf16 8"])
 @pytest.mark.parametrize("way", WAYS, ids=lambda w: w[0])
 def test_small_weights_by_every_launch(way, kind, gap, wide):
